@@ -74,8 +74,14 @@ enum { RLK_AGG_SEQ_MEAN_TOKEN_MEAN = 0, RLK_AGG_TOKEN_MEAN = 1 };
 enum {
   RLK_DERR_TARGET = 1,       /* a policy row's target lies outside [0, V) */
   RLK_DERR_CU_SEQLENS = 2,   /* cu[0] != 0, cu decreasing, or cu[R] != N */
-  RLK_DERR_POLICY_BOUND = 4  /* more trained tokens than rlk_batch_t.max_policy_tokens; the
+  RLK_DERR_POLICY_BOUND = 4, /* more trained tokens than rlk_batch_t.max_policy_tokens; the
                                 outputs of that call are not valid */
+  RLK_DERR_KV_LEN = 8,       /* kv_len[b] below the sequence's new tokens, or above its pages or its row
+                                of slot_end; the sequence's rows are left as they were */
+  RLK_DERR_PAGE = 16,        /* a page index in use lies outside [0, n_pages): nothing is appended
+                                there, and rows that read it are not valid */
+  RLK_DERR_LOGITS = 32       /* a row of logits that decides a token holds NaN or +inf, or nothing
+                                above -inf; the sequence's outputs are not valid */
 };
 
 /* Size limits: the GEMMs address 256-row operand panels with 32-bit buffer offsets, so a
@@ -326,6 +332,116 @@ typedef struct {
 } rlk_tree_out_t;
 
 rlk_status_t rlk_tree_pack(const rlk_calls_t* calls, rlk_tree_out_t* out);
+
+/* Where every packed position's subtree ends: the position after the last one that descends from it.
+ * In the depth-first packing of rlk_tree_pack position j lies on the root path of position i (i's
+ * token comes after j's in one trajectory) exactly when j <= i < end[j], which is the visibility that
+ * rlk_kv_attention takes.  Host code, host pointers: pos_off [R+1] and parent as rlk_tree_pack writes
+ * them; parent[i] (batch-global) must lie in i's rollout and before i, or be -1.  end [pos_off[R]] is
+ * counted from the rollout's first position (the position's slot when the rollout is one sequence of a
+ * cache).  With parents of any other depth-first tree, e.g. of drafted branches, it does the same. */
+rlk_status_t rlk_tree_ends(int32_t R, const int64_t* pos_off, const int32_t* parent, int32_t* end);
+
+/* ---- The rollout side: the pass that makes the tokens and the log-probs the loss takes ----
+ * A rollout's keys and values live in a paged cache; each model call appends a chunk of new tokens (a
+ * prompt, a tool's output, drafted tokens, one token), attends over the cache and samples.  The same two
+ * calls evaluate packed prefix trees (rlk_tree_pack) chunk by chunk: the position of a token is then its
+ * depth, and rlk_tree_ends says what it sees. */
+typedef struct {
+  int64_t T;                  /* rows of q, k, v and of their outputs: the sequences' new tokens back to
+                                 back; rows from cu_new[B] on are left as they were */
+  int32_t B;                  /* sequences, at most 16384 */
+  int32_t n_pages;            /* pages of the pools; offsets pass 32 bits */
+  int32_t page_size;          /* tokens of a page: a power of two, 1 .. 1024 */
+  int32_t max_pages;          /* columns of page_table */
+  int32_t n_q_heads;          /* query heads, a multiple of n_kv_heads, at most 128 to a key head; query
+                                 head h reads key head h / (n_q_heads / n_kv_heads) */
+  int32_t n_kv_heads;
+  int32_t head_dim;           /* multiple of 8, 8 .. 256 */
+  int32_t dtype;              /* of q, k, v, the pools and the outputs: RLK_DTYPE_F32 or RLK_DTYPE_BF16 */
+  void* k_pages;              /* [n_pages, n_kv_heads, page_size, head_dim], 16-byte aligned */
+  void* v_pages;              /* the same */
+  const int32_t* page_table;  /* [B, max_pages]: slot s of sequence b lies in page page_table[b, s / page_size];
+                                 only the entries of slots below kv_len[b] are read */
+  const int32_t* kv_len;      /* [B]: tokens held, the new ones included */
+  const int32_t* cu_new;      /* [B+1]: the new tokens of sequence b are rows cu_new[b] .. cu_new[b+1] - 1 and
+                                 take the last slots below kv_len[b]; cu_new[0] = 0, non-decreasing, cu_new[B]
+                                 at most T */
+  int32_t max_new;            /* optional host-known largest count of new tokens of a sequence (0 = unknown);
+                                 it plans the attention's tiles, the results hold for any value */
+  int32_t reserved;           /* 0 */
+} rlk_kv_t;
+
+/* Rotation pairs: element i with i + rot_dim / 2 (HALF), or 2 i with 2 i + 1 (PAIRS). */
+enum { RLK_ROT_HALF = 0, RLK_ROT_PAIRS = 1 };
+
+typedef struct {
+  const double* freq;    /* device [rot_dim / 2]: angle per position of each pair (radians); NULL with rot_dim 0 */
+  int32_t rot_dim;       /* leading elements of a head that are rotated: 0 (none), or up to head_dim and a
+                            multiple of 16 (HALF) or 8 (PAIRS) */
+  int32_t rot_style;     /* RLK_ROT_* */
+  const void* q_norm;    /* device [head_dim] in the cache's dtype: weights of the RMS norm of each query head
+                            (16-byte aligned); NULL = no norm */
+  const void* k_norm;    /* the same for each key head */
+  float norm_eps;        /* added to the mean square; >= 0 */
+  int32_t reserved;      /* 0 */
+} rlk_rot_t;
+
+/* Workspace bytes of rlk_kv_append and rlk_kv_attention for this cache (one size for both).  Host
+ * pointers; device pointers of the descriptor are not read. */
+rlk_status_t rlk_kv_workspace_size(const rlk_kv_t* c, size_t* bytes);
+
+/* Appends the chunk's keys and values to the cache and makes its queries ready, in one pass: per token,
+ * x' = norm(x) for every query and key head, (a, b) -> (a cos - b sin, b cos + a sin) on its pairs at the
+ * angle position * freq, keys and values written to the token's slot, queries to q_out.
+ * q [T, n_q_heads, head_dim], k and v [T, n_kv_heads, head_dim]: heads contiguous, q_stride / k_stride /
+ * v_stride elements from token to token (multiples of 8; views into one fused projection are fine), 16-byte
+ * aligned.  positions [T] device or NULL (the position is the slot).  q_out [T, n_q_heads, head_dim]
+ * contiguous; it may be q itself when q is contiguous.  q and q_out may both be NULL (keys and values only).
+ * Norms and rotations are computed in fp32 and rounded once; angles are reduced in fp64, so far positions
+ * lose nothing.  Pages that take new tokens must not be shared by two sequences of the call. */
+rlk_status_t rlk_kv_append(const rlk_kv_t* c, const rlk_rot_t* r, const void* q, int64_t q_stride, const void* k,
+                           int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions, void* q_out,
+                           void* ws, size_t ws_bytes, void* stream);
+
+/* Attention of the chunk's tokens over the cache (which holds them already): the token in slot s of its
+ * sequence sees the slots j <= s, with slot_end (device int32 [B, end_stride], end_stride at least the
+ * largest kv_len) only those with s < slot_end[b, j] too.  out [T, n_q_heads, head_dim] = softmax(scale q
+ * k^T) v over what the token sees, lse [T, n_q_heads] fp32 (may be NULL) = log of the sum of exp(scale q k^T).
+ * A token that sees nothing gets out = 0 and lse = -inf.  q [T, n_q_heads, head_dim] with q_stride elements
+ * from token to token (a multiple of 8), q and out 16-byte aligned; out must not overlap q or the pools.
+ * scale finite.  Pages may be shared between sequences.  Softmax statistics and sums are fp32.  Results are
+ * the same from call to call (fixed order of the sums).  Values in slots below kv_len that a token does not
+ * see do not reach its row, whatever they are; slots from kv_len on are not read. */
+rlk_status_t rlk_kv_attention(const rlk_kv_t* c, const void* q, int64_t q_stride, const int32_t* slot_end,
+                              int64_t end_stride, float scale, void* out, float* lse, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/* Verification of drafted tokens against the target's probabilities, from given random numbers.
+ * Sequence b has n_b = cu_draft[b+1] - cu_draft[b] drafts (>= 0) and n_b + 1 rows: row cu_draft[b] + b + i
+ * of logits is the target's distribution of the token after i accepted drafts.  With p = softmax(logits /
+ * temperature) and q = softmax(draft_logits / temperature) (draft_logits NULL: q is 1 at the drafted token,
+ * e.g. the text of an earlier rollout), draft i with token y is accepted while u_accept[i] q(y) < p(y).  At
+ * the first draft that is not, the token is drawn from max(p - q, 0) (from p where that is nothing, as with a
+ * draft that neither gives any mass), otherwise from the last row's p: the lowest token whose cumulative mass
+ * (in token order) exceeds u_sample[b] times the whole.
+ * Outputs by row: tokens (accepted drafts, then the drawn token, then -1) and logp, log p of each emitted token
+ * (0 elsewhere), which is the log-prob that the loss takes as rollout_logp or old_logp; n_accepted [B].
+ * Rows from cu_draft[B] + B on are left as they were.  Logits of -inf have no mass.  Sums and decisions are fp64. */
+typedef struct {
+  int64_t n_draft;     /* rows of draft, u_accept and draft_logits; logits, tokens and logp have n_draft + B */
+  int32_t B;           /* sequences, at most 16384 */
+  int32_t V;           /* vocabulary, 1 .. RLK_MAX_DIM */
+  int32_t dtype;       /* of both logits */
+  float temperature;   /* 0 means 1 (the default); otherwise finite and > 0 */
+  int64_t ld_logits;   /* elements from row to row, at least V */
+  int64_t ld_draft;
+} rlk_verify_t;
+
+rlk_status_t rlk_verify_workspace_size(const rlk_verify_t* p, size_t* bytes);
+rlk_status_t rlk_draft_verify(const rlk_verify_t* p, const void* logits, const void* draft_logits, const int32_t* draft,
+                              const int32_t* cu_draft, const float* u_accept, const float* u_sample, int32_t* tokens,
+                              int32_t* n_accepted, float* logp, void* ws, size_t ws_bytes, void* stream);
 
 /* Synchronises `stream`, then reads the status word that the previous calls using `ws`
  * left there.  *flags (optional host pointer) receives RLK_DERR_* bits; returns RLK_OK or

@@ -26,3 +26,4 @@ from .rl_oracle import (  # noqa: F401
     value_head_grads,
     tree_pack,
 )
+from . import rollout_oracle as rollout  # noqa: F401

@@ -18,13 +18,16 @@ RLK_OK, RLK_EINVAL, RLK_ESHAPE, RLK_EDTYPE, RLK_EWORKSPACE, RLK_EHIP, RLK_EDATA 
 DTYPE_F32, DTYPE_BF16 = 0, 1
 AGG_SEQ, AGG_TOKEN = 0, 1
 DERR_TARGET, DERR_CU_SEQLENS, DERR_POLICY_BOUND = 1, 2, 4
+DERR_KV_LEN, DERR_PAGE, DERR_LOGITS = 8, 16, 32
+ROT_HALF, ROT_PAIRS = 0, 1
 
 EXPORTS = [
     "rlk_workspace_size", "rlk_advantage_workspace_size", "rlk_compact", "rlk_logprob_fwd", "rlk_group_advantage",
     "rlk_pg_loss_fwd_bwd", "rlk_check_status", "rlk_status_string", "rlk_last_error", "rlk_version",
     "rlk_profile_begin", "rlk_profile_end", "rlk_kernel_kind_name", "rlk_gae", "rlk_value_workspace_size",
     "rlk_value_loss", "rlk_tree_pack", "rlk_value_head_fwd", "rlk_value_head_workspace_size", "rlk_value_head_bwd",
-    "rlk_group_advantage_noalloc",
+    "rlk_group_advantage_noalloc", "rlk_tree_ends", "rlk_kv_workspace_size", "rlk_kv_append", "rlk_kv_attention",
+    "rlk_verify_workspace_size", "rlk_draft_verify",
 ]
 
 
@@ -61,6 +64,26 @@ class TreeOut(ctypes.Structure):
                 ("row_src", ctypes.c_void_p), ("row_target", ctypes.c_void_p), ("row_mask", ctypes.c_void_p),
                 ("row_cu", ctypes.c_void_p), ("leaves", ctypes.c_void_p), ("n_pos", ctypes.c_int64),
                 ("n_rows", ctypes.c_int64)]
+
+
+class KvCache(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("B", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("cu_new", ctypes.c_void_p), ("max_new", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("rot_style", ctypes.c_int32),
+                ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("norm_eps", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
+class Verify(ctypes.Structure):
+    _fields_ = [("n_draft", ctypes.c_int64), ("B", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("temperature", ctypes.c_float), ("ld_logits", ctypes.c_int64), ("ld_draft", ctypes.c_int64)]
 
 
 class RlkError(RuntimeError):
@@ -108,6 +131,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.rlk_value_head_fwd.argtypes = [ctypes.POINTER(Batch), vp, vp, f32, vp, vp, vp, vp]
     lib.rlk_value_head_workspace_size.argtypes = [ctypes.POINTER(Batch), ctypes.POINTER(sz)]
     lib.rlk_value_head_bwd.argtypes = [ctypes.POINTER(Batch), vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.rlk_tree_ends.argtypes = [i32, vp, vp, vp]
+    pk, pr, pv = ctypes.POINTER(KvCache), ctypes.POINTER(Rotation), ctypes.POINTER(Verify)
+    lib.rlk_kv_workspace_size.argtypes = [pk, ctypes.POINTER(sz)]
+    lib.rlk_kv_append.argtypes = [pk, pr, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    lib.rlk_kv_attention.argtypes = [pk, vp, i64, vp, i64, f32, vp, vp, vp, sz, vp]
+    lib.rlk_verify_workspace_size.argtypes = [pv, ctypes.POINTER(sz)]
+    lib.rlk_draft_verify.argtypes = [pv, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.rlk_kernel_kind_name.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("rlk_status_string", "rlk_last_error", "rlk_kernel_kind_name", "rlk_version"):
@@ -671,6 +701,203 @@ def tree_pack(calls_per_rollout, cap_pos=None, cap_rows=None) -> dict:
         out[k] = out[k][:o.n_rows]
     out["leaves"] = out["leaves"][:R]
     return out
+
+
+def tree_ends(pos_off, parent):
+    """Where every packed position's subtree ends, counted from its rollout's first position (see rlk_tree_ends):
+    position i of a rollout sees position j exactly when j <= i < end[j].  Takes tree_pack's pos_off and parent;
+    host numpy array of int32."""
+    import numpy as np
+
+    pos_off = np.ascontiguousarray(pos_off, dtype=np.int64)
+    parent = np.ascontiguousarray(parent, dtype=np.int32)
+    if pos_off.ndim != 1 or pos_off.size < 1 or parent.ndim != 1:
+        raise ValueError("pos_off needs R + 1 >= 1 entries and parent one per position")
+    if pos_off[-1] != parent.size:
+        raise ValueError(f"pos_off ends at {pos_off[-1]}, parent has {parent.size} positions")
+    end = np.zeros(max(parent.size, 1), np.int32)
+    _check(load_library().rlk_tree_ends(pos_off.size - 1, pos_off.ctypes.data, parent.ctypes.data, end.ctypes.data))
+    return end[:parent.size]
+
+
+def _token_rows(t, name: str, heads, dim, dtype, tokens=None):
+    """A [tokens, heads, dim] tensor whose heads lie together; the tokens may be any stride apart (a view into a
+    fused projection).  Returns the stride in elements."""
+    import torch
+
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    want = (tokens, heads, dim)
+    if t.dim() != 3 or any(w is not None and int(a) != int(w) for a, w in zip(t.shape, want)):
+        raise ValueError(f"{name} has shape {list(t.shape)}, expected "
+                         f"[{', '.join('*' if w is None else str(int(w)) for w in want)}]")
+    n, h, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
+        raise ValueError(f"{name} must hold the heads of a token together (strides {list(t.stride())})")
+    return t.stride(0) if n > 1 else h * d
+
+
+def _check_cache(k_pages, v_pages, page_table, kv_len, cu_new):
+    """The cache tensors shared by kv_append and kv_attention; returns (B, Hkv, page_size, D)."""
+    import torch
+
+    i32 = (torch.int32,)
+    _tensor(k_pages, "k_pages", shape=(None, None, None, None), dtypes=_float_types())
+    _tensor(v_pages, "v_pages", shape=k_pages.shape, dtypes=(k_pages.dtype,))
+    _tensor(kv_len, "kv_len", shape=(None,), dtypes=i32)
+    B = kv_len.shape[0]
+    _tensor(page_table, "page_table", shape=(B, None), dtypes=i32)
+    _tensor(cu_new, "cu_new", shape=(B + 1,), dtypes=i32)
+    return B, k_pages.shape[1], k_pages.shape[2], k_pages.shape[3]
+
+
+def make_cache(k_pages, v_pages, page_table, kv_len, cu_new, T, n_q_heads, max_new: int = 0) -> KvCache:
+    """Cache descriptor (rlk_kv_t); max_new is an optional host-known bound on a sequence's new tokens."""
+    n_pages, n_kv_heads, page_size, head_dim = k_pages.shape
+    return KvCache(T=T, B=kv_len.shape[0], n_pages=n_pages, page_size=page_size, max_pages=page_table.shape[1],
+                   n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=_dtype_code(k_pages),
+                   k_pages=_ptr(k_pages), v_pages=_ptr(v_pages), page_table=_ptr(page_table), kv_len=_ptr(kv_len),
+                   cu_new=_ptr(cu_new), max_new=int(max_new))
+
+
+def kv_workspace_size(cache: KvCache) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().rlk_kv_workspace_size(ctypes.byref(cache), ctypes.byref(n)))
+    return n.value
+
+
+def _gpu_scope(device):
+    """Makes `device` current for a launch (the current stream is that device's then)."""
+    import torch
+
+    return torch.cuda.device(device)
+
+
+def kv_append(k_pages, v_pages, page_table, kv_len, cu_new, q, k, v, freq=None, positions=None, q_norm=None, k_norm=None,
+              norm_eps: float = 1e-6, rot_style: str = "half", q_out=None, ws=None, stream=None):
+    """Appends new tokens' keys and values to the paged cache, normed and rotated on the way, and makes their
+    queries ready (see rlk_kv_append).  q [T, Hq, D] (or None), k and v [T, Hkv, D]: heads of a token together, so
+    views into one fused projection are fine; freq [rot_dim / 2] fp64: angle per position (None: no rotation);
+    kv_len counts the new tokens.  Returns (q_out, ws)."""
+    import torch
+
+    B, Hkv, _, D = _check_cache(k_pages, v_pages, page_table, kv_len, cu_new)
+    dt = k_pages.dtype
+    ks = _token_rows(k, "k", Hkv, D, dt)
+    T = k.shape[0]
+    vs = _token_rows(v, "v", Hkv, D, dt, T)
+    qs, Hq = 0, Hkv
+    if q is not None:
+        qs = _token_rows(q, "q", None, D, dt, T)
+        Hq = q.shape[1]
+        _tensor(q_out, "q_out", shape=(T, Hq, D), dtypes=(dt,), optional=True)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _tensor(freq, "freq", shape=(None,), dtypes=(torch.float64,), optional=True)
+    _tensor(positions, "positions", shape=(T,), dtypes=(torch.int32,), optional=True)
+    _tensor(q_norm, "q_norm", shape=(D,), dtypes=(dt,), optional=True)
+    _tensor(k_norm, "k_norm", shape=(D,), dtypes=(dt,), optional=True)
+    _tensor(ws, "ws", dtypes=(torch.uint8,), optional=True)
+    if rot_style not in ("half", "pairs"):
+        raise ValueError(f"rot_style must be 'half' or 'pairs', got {rot_style!r}")
+    _on_one_gpu(k_pages=k_pages, v_pages=v_pages, page_table=page_table, kv_len=kv_len, cu_new=cu_new, q=q, k=k, v=v,
+                freq=freq, positions=positions, q_norm=q_norm, k_norm=k_norm, q_out=q_out, ws=ws)
+    lib = load_library()
+    c = make_cache(k_pages, v_pages, page_table, kv_len, cu_new, T, Hq)
+    r = Rotation(freq=_ptr(freq), rot_dim=0 if freq is None else 2 * freq.shape[0],
+                 rot_style=ROT_PAIRS if rot_style == "pairs" else ROT_HALF, q_norm=_ptr(q_norm), k_norm=_ptr(k_norm),
+                 norm_eps=norm_eps)
+    if q is not None and q_out is None:
+        q_out = torch.empty(T, Hq, D, dtype=dt, device=q.device)
+    if ws is None:
+        ws = alloc_workspace(kv_workspace_size(c), k_pages.device)
+    with _gpu_scope(k_pages.device):
+        _check(lib.rlk_kv_append(ctypes.byref(c), ctypes.byref(r), _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(positions),
+                                 _ptr(q_out), _ptr(ws), ws.numel(), _stream_handle(stream)))
+    return q_out, ws
+
+
+def kv_attention(q, k_pages, v_pages, page_table, kv_len, cu_new, scale=None, slot_end=None, max_new: int = 0, out=None,
+                 lse=None, ws=None, stream=None):
+    """Attention of the sequences' new tokens over the paged cache that holds them already (see rlk_kv_attention).
+    q [T, Hq, D] as kv_append made it; scale defaults to D^-1/2; slot_end [B, >= largest kv_len] int32 (tree_ends per
+    sequence): a token in slot s sees slot j only while s < slot_end[b, j]; max_new: optional host-known bound on a
+    sequence's new tokens; lse [T, Hq] fp32 is written when given.  Returns (out, lse, ws)."""
+    import torch
+
+    B, Hkv, _, D = _check_cache(k_pages, v_pages, page_table, kv_len, cu_new)
+    dt = k_pages.dtype
+    qs = _token_rows(q, "q", None, D, dt)
+    T, Hq = q.shape[0], q.shape[1]
+    _tensor(slot_end, "slot_end", shape=(B, None), dtypes=(torch.int32,), optional=True)
+    _tensor(out, "out", shape=(T, Hq, D), dtypes=(dt,), optional=True)
+    _tensor(lse, "lse", shape=(T, Hq), dtypes=(torch.float32,), optional=True)
+    _tensor(ws, "ws", dtypes=(torch.uint8,), optional=True)
+    _on_one_gpu(q=q, k_pages=k_pages, v_pages=v_pages, page_table=page_table, kv_len=kv_len, cu_new=cu_new,
+                slot_end=slot_end, out=out, lse=lse, ws=ws)
+    lib = load_library()
+    c = make_cache(k_pages, v_pages, page_table, kv_len, cu_new, T, Hq, max_new)
+    if out is None:
+        out = torch.empty(T, Hq, D, dtype=dt, device=q.device)
+    if ws is None:
+        ws = alloc_workspace(kv_workspace_size(c), q.device)
+    with _gpu_scope(q.device):
+        _check(lib.rlk_kv_attention(ctypes.byref(c), _ptr(q), qs, _ptr(slot_end),
+                                    0 if slot_end is None else slot_end.shape[1], D ** -0.5 if scale is None else scale,
+                                    _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream_handle(stream)))
+    return out, lse, ws
+
+
+def verify_workspace_size(p: Verify) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().rlk_verify_workspace_size(ctypes.byref(p), ctypes.byref(n)))
+    return n.value
+
+
+def draft_verify(logits, draft, cu_draft, u_accept, u_sample, draft_logits=None, temperature: float = 1.0, tokens=None,
+                 n_accepted=None, logp=None, ws=None, stream=None):
+    """Verification of drafted tokens from given random numbers (see rlk_draft_verify).  logits [n_draft + B, V] of the
+    target (a sequence's drafts and one row more), draft [n_draft] int32, cu_draft [B + 1] int32, u_accept [n_draft] and
+    u_sample [B] fp32 in [0, 1), draft_logits [n_draft, V] or None (drafts without probabilities).  Returns (tokens,
+    n_accepted, logp, ws); tokens and logp by row of logits, -1 and 0 behind a sequence's drawn token."""
+    import torch
+
+    i32, f32 = (torch.int32,), (torch.float32,)
+    _tensor(logits, "logits", shape=(None, None), dtypes=_float_types())
+    rows, V = logits.shape
+    _tensor(draft, "draft", shape=(None,), dtypes=i32)
+    n = draft.shape[0]
+    _tensor(u_sample, "u_sample", shape=(None,), dtypes=f32)
+    B = u_sample.shape[0]
+    if rows != n + B:
+        raise ValueError(f"logits has {rows} rows, expected n_draft + B = {n + B}")
+    _tensor(cu_draft, "cu_draft", shape=(B + 1,), dtypes=i32)
+    _tensor(u_accept, "u_accept", shape=(n,), dtypes=f32)
+    _tensor(draft_logits, "draft_logits", shape=(n, V), dtypes=(logits.dtype,), optional=True)
+    _tensor(tokens, "tokens", shape=(rows,), dtypes=i32, optional=True)
+    _tensor(n_accepted, "n_accepted", shape=(B,), dtypes=i32, optional=True)
+    _tensor(logp, "logp", shape=(rows,), dtypes=f32, optional=True)
+    _tensor(ws, "ws", dtypes=(torch.uint8,), optional=True)
+    _on_one_gpu(logits=logits, draft=draft, cu_draft=cu_draft, u_accept=u_accept, u_sample=u_sample,
+                draft_logits=draft_logits, tokens=tokens, n_accepted=n_accepted, logp=logp, ws=ws)
+    lib = load_library()
+    dev = logits.device
+    p = Verify(n_draft=n, B=B, V=V, dtype=_dtype_code(logits), temperature=temperature, ld_logits=V, ld_draft=V)
+    if tokens is None:
+        tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+    if n_accepted is None:
+        n_accepted = torch.empty(B, dtype=torch.int32, device=dev)
+    if logp is None:
+        logp = torch.empty(rows, dtype=torch.float32, device=dev)
+    if ws is None:
+        ws = alloc_workspace(verify_workspace_size(p), dev)
+    with _gpu_scope(dev):
+        _check(lib.rlk_draft_verify(ctypes.byref(p), _ptr(logits), _ptr(draft_logits), _ptr(draft), _ptr(cu_draft),
+                                    _ptr(u_accept), _ptr(u_sample), _ptr(tokens), _ptr(n_accepted), _ptr(logp), _ptr(ws),
+                                    ws.numel(), _stream_handle(stream)))
+    return tokens, n_accepted, logp, ws
 
 
 def check_status(ws, stream=None) -> int:

@@ -1,0 +1,335 @@
+// Rollout side: the append of a chunk of new tokens to the paged key/value cache (per-head norm and position
+// rotation on the way) and the chunk's attention over the cache.
+//
+// Pools are [n_pages, n_kv_heads, page_size, head_dim]: the keys of one head in a page lie together, so an
+// attention workgroup streams whole lines.  A workgroup never trusts device data: sequences whose offsets or
+// lengths do not fit are skipped, page indices outside the pool are not followed, and both set status bits.
+#include "rlk_internal.h"
+
+#include <math.h>
+
+namespace rlk {
+
+namespace {
+
+__device__ __forceinline__ float bf16_to_f(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
+
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+  bf16x2 v;
+  v.x = (__bf16)lo;
+  v.y = (__bf16)hi;
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// elements of a 16-byte chunk
+template <typename T>
+constexpr int kEpc = 16 / (int)sizeof(T);
+
+template <typename T>
+__device__ __forceinline__ void unpack(u32x4 v, float* f) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      f[2 * i] = __uint_as_float(v[i] << 16);
+      f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    } else {
+      f[i] = __uint_as_float(v[i]);
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ u32x4 pack(const float* f) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) v[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+    else v[i] = __float_as_uint(f[i]);
+  }
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ float load1(const T* p) {
+  if constexpr (sizeof(T) == 2) return bf16_to_f(p->bits);
+  else return *p;
+}
+
+// Rows, count and length of sequence b: n = 0 where the sequence is empty or its numbers do not fit.
+struct Seq {
+  int row0, n, len;
+};
+__device__ __forceinline__ Seq sequence(const KvArgs& a, int b, int* bad = nullptr) {
+  const int r0 = a.cu[b], r1 = a.cu[b + 1], len = a.kv_len[b];
+  const bool rows = r0 >= 0 && r1 >= r0 && r1 <= a.T;
+  const bool fits = len >= 0 && len <= a.cap && (!rows || len >= r1 - r0);
+  if (bad) *bad |= (rows ? 0 : RLK_DERR_CU_SEQLENS) | (fits ? 0 : RLK_DERR_KV_LEN);
+  return {r0, rows && fits ? r1 - r0 : 0, len};
+}
+
+// Status bits of the whole call, by one workgroup: offsets, lengths and the pages of the slots from `first` new
+// token (append) or from slot 0 (attention) on.
+__device__ void check_cache(const KvArgs& a, bool new_only, int32_t* status) {
+  __shared__ int s_bad;
+  if (threadIdx.x == 0) s_bad = 0;
+  __syncthreads();
+  int bad = 0;
+  if (threadIdx.x == 0 && a.cu[0] != 0) bad |= RLK_DERR_CU_SEQLENS;
+  const int lane = threadIdx.x & 63, nw = blockDim.x >> 6;
+  for (int b = threadIdx.x >> 6; b < a.B; b += nw) {
+    const Seq s = sequence(a, b, &bad);
+    if (s.n == 0) continue;
+    const int p0 = new_only ? (s.len - s.n) >> a.ps_shift : 0, p1 = (s.len - 1) >> a.ps_shift;
+    for (int p = p0 + lane; p <= p1; p += 64)
+      if ((uint32_t)a.table[(int64_t)b * a.max_pages + p] >= (uint32_t)a.n_pages) bad |= RLK_DERR_PAGE;
+  }
+  if (bad) atomicOr(&s_bad, bad);
+  __syncthreads();
+  if (threadIdx.x == 0) *status = s_bad;
+}
+
+// ---------------------------------------------------------------- append
+
+constexpr int kAppendTokens = 4;   // most tokens of a workgroup
+constexpr int kAppendBatch = 4;    // 16-byte chunks a lane has in flight
+
+// A workgroup takes `tpb` consecutive tokens.  A head is a group of 2^lg lanes, 16 bytes each, so the norm's sum
+// stays within the group and the HALF partner of an element is the same element of another lane.  The angles'
+// sines and cosines, the same for every head, are made once per token and read from LDS.  The last workgroup only
+// checks.  Bound by memory: every element is read and written once.
+template <typename T>
+__global__ void __launch_bounds__(256) k_kv_append(KvArgs a, RotArgs r, int lg, int tpb, int32_t* status) {
+  constexpr int EPC = kEpc<T>;
+  if (blockIdx.x == gridDim.x - 1) {
+    check_cache(a, true, status);
+    return;
+  }
+  __shared__ float2 s_cs[kAppendTokens][128];
+  __shared__ int s_cnt[4][kAppendTokens];
+  __shared__ int s_pos[kAppendTokens];
+  __shared__ int64_t s_at[kAppendTokens];  // first element of the slot in its page's head 0; -1: no slot, -2: no row
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int64_t t0 = (int64_t)blockIdx.x * tpb;
+  int cnt[kAppendTokens] = {};
+  for (int b = tid; b < a.B; b += 256) {
+    const int c = a.cu[b + 1];
+#pragma unroll
+    for (int j = 0; j < kAppendTokens; ++j) cnt[j] += c <= t0 + j;
+  }
+#pragma unroll
+  for (int j = 0; j < kAppendTokens; ++j) {
+    for (int o = 32; o > 0; o >>= 1) cnt[j] += __shfl_xor(cnt[j], o, 64);
+    if (lane == 0) s_cnt[w][j] = cnt[j];
+  }
+  __syncthreads();
+  if (tid < tpb) {
+    const int64_t t = t0 + tid;
+    const int b = s_cnt[0][tid] + s_cnt[1][tid] + s_cnt[2][tid] + s_cnt[3][tid];
+    int64_t at = -2;
+    int pos = 0;
+    if (t < a.T && b < a.B) {
+      const Seq s = sequence(a, b);
+      const int64_t i = t - s.row0;
+      if (i >= 0 && i < s.n) {
+        const int slot = s.len - s.n + (int)i;
+        const int page = a.table[(int64_t)b * a.max_pages + (slot >> a.ps_shift)];
+        pos = r.positions ? r.positions[t] : slot;
+        at = (uint32_t)page < (uint32_t)a.n_pages
+                 ? ((int64_t)page * a.Hkv << a.ps_shift) * a.D + (int64_t)(slot & ((1 << a.ps_shift) - 1)) * a.D
+                 : -1;
+      }
+    }
+    s_at[tid] = at;
+    s_pos[tid] = pos;
+  }
+  __syncthreads();
+  const int half = r.rot / 2;
+  for (int i = tid; i < tpb * half; i += 256) {
+    const int j = i / half, f = i - j * half;
+    // whole turns are taken off in fp64: an angle of 1e6 radians keeps 1e-10
+    double turn = (double)s_pos[j] * r.freq[f] * 0.15915494309189535;
+    turn -= rint(turn);
+    float sn, cs;
+    sincospif(2.0f * (float)turn, &sn, &cs);
+    s_cs[j][f] = make_float2(cs, sn);
+  }
+  __syncthreads();
+
+  const int hpw = 64 >> lg, sub = lane >> lg, ch = lane & ((1 << lg) - 1);
+  const int Hq = r.q ? a.Hq : 0, NH = Hq + 2 * a.Hkv;
+  const int ipt = (NH + hpw - 1) / hpw, items = ipt * tpb;
+  const bool on = ch * EPC < a.D;
+  const int shift = half / EPC;  // HALF: lanes to the partner
+  const bool turns = ch * EPC < r.rot;
+  const bool first = ch < shift;
+  float wq[EPC], wk[EPC];
+  if (r.q_norm && on) unpack<T>(*reinterpret_cast<const u32x4*>((const T*)r.q_norm + ch * EPC), wq);
+  if (r.k_norm && on) unpack<T>(*reinterpret_cast<const u32x4*>((const T*)r.k_norm + ch * EPC), wk);
+  const float inv_d = 1.0f / (float)a.D;
+  const int64_t head_step = (int64_t)a.D << a.ps_shift;
+
+  for (int i0 = w; i0 < items; i0 += 4 * kAppendBatch) {
+    u32x4 x[kAppendBatch];
+#pragma unroll
+    for (int u = 0; u < kAppendBatch; ++u) {
+      const int it = i0 + 4 * u, j = it / ipt, h = (it - j * ipt) * hpw + sub;
+      x[u] = u32x4{0, 0, 0, 0};
+      if (it < items && on && h < NH && s_at[j] != -2) {
+        const int64_t t = t0 + j;
+        const T* p = h < Hq ? (const T*)r.q + t * r.q_stride + (int64_t)h * a.D
+                     : h < Hq + a.Hkv ? (const T*)r.k + t * r.k_stride + (int64_t)(h - Hq) * a.D
+                                      : (const T*)r.v + t * r.v_stride + (int64_t)(h - Hq - a.Hkv) * a.D;
+        x[u] = *reinterpret_cast<const u32x4*>(p + ch * EPC);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAppendBatch; ++u) {
+      const int it = i0 + 4 * u, j = it / ipt, h = (it - j * ipt) * hpw + sub;
+      if (it >= items) break;  // the same for the whole wavefront
+      const int64_t at = s_at[j];
+      float f[EPC];
+      unpack<T>(x[u], f);
+      const bool is_q = h < Hq, is_v = h >= Hq + a.Hkv;
+      if (r.q_norm || r.k_norm) {
+        float ss = 0.0f;
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) ss += f[e] * f[e];
+        for (int o = 1; o < (1 << lg); o <<= 1) ss += __shfl_xor(ss, o, 64);
+        const void* nw = is_q ? r.q_norm : is_v ? nullptr : r.k_norm;
+        if (nw) {
+          const float sc = rsqrtf(ss * inv_d + r.eps);
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) f[e] = f[e] * sc * (is_q ? wq[e] : wk[e]);
+        }
+      }
+      if (r.rot > 0) {
+        float y[EPC];
+        if (r.pairs) {
+#pragma unroll
+          for (int e = 0; e < EPC; e += 2) {
+            const float2 cs = turns ? s_cs[j][(ch * EPC + e) >> 1] : make_float2(1.0f, 0.0f);
+            y[e] = f[e] * cs.x - f[e + 1] * cs.y;
+            y[e + 1] = f[e + 1] * cs.x + f[e] * cs.y;
+          }
+        } else {
+          const int from = turns ? (first ? lane + shift : lane - shift) : lane;
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) {
+            const float o = __shfl(f[e], from, 64);
+            const float2 cs = turns ? s_cs[j][(first ? ch : ch - shift) * EPC + e] : make_float2(1.0f, 0.0f);
+            y[e] = first ? f[e] * cs.x - o * cs.y : f[e] * cs.x + o * cs.y;
+          }
+        }
+        if (turns && !is_v) {
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) f[e] = y[e];
+        }
+      }
+      if (!on || h >= NH || at == -2) continue;
+      const u32x4 out = is_v ? x[u] : pack<T>(f);
+      if (is_q) {
+        *reinterpret_cast<u32x4*>((T*)r.q_out + ((t0 + j) * a.Hq + h) * a.D + ch * EPC) = out;
+      } else if (at >= 0) {
+        T* pool = is_v ? (T*)a.v_pages : (T*)a.k_pages;
+        const int kh = is_v ? h - Hq - a.Hkv : h - Hq;
+        *reinterpret_cast<u32x4*>(pool + at + kh * head_step + ch * EPC) = out;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- attention
+
+__global__ void __launch_bounds__(1024) k_kv_check(KvArgs a, int32_t* status) { check_cache(a, false, status); }
+
+// One wavefront per token and query head, 64 keys at a time: a lane scores a key, then adds up its share of the
+// head's elements.
+template <typename T>
+__global__ void __launch_bounds__(64) k_kv_attention(KvArgs a, AttnArgs p) {
+  __shared__ float s_q[256];
+  __shared__ float s_p[64];
+  __shared__ int s_b;
+  const int64_t t = blockIdx.x;
+  const int h = blockIdx.y, lane = threadIdx.x;
+  int cnt = 0;
+  for (int b = lane; b < a.B; b += 64) cnt += a.cu[b + 1] <= t;
+  for (int o = 32; o > 0; o >>= 1) cnt += __shfl_xor(cnt, o, 64);
+  if (cnt >= a.B) return;
+  const Seq s = sequence(a, cnt);
+  const int64_t i = t - s.row0;
+  if (i < 0 || i >= s.n) return;
+  const int slot = s.len - s.n + (int)i, kh = h / (a.Hq / a.Hkv);
+  for (int e = lane; e < a.D; e += 64) s_q[e] = load1((const T*)p.q + t * p.q_stride + (int64_t)h * a.D + e);
+  __syncthreads();
+  float m = -INFINITY, l = 0.0f, acc[4] = {};
+  const int64_t head_step = (int64_t)a.D << a.ps_shift;
+  for (int j0 = 0; j0 <= slot; j0 += 64) {
+    const int j = j0 + lane;
+    bool see = j <= slot;
+    int64_t at = 0;
+    if (see) {
+      const int page = a.table[(int64_t)cnt * a.max_pages + (j >> a.ps_shift)];
+      if ((uint32_t)page >= (uint32_t)a.n_pages) see = false;
+      else at = (int64_t)page * a.Hkv * head_step + kh * head_step + (int64_t)(j & ((1 << a.ps_shift) - 1)) * a.D;
+      if (p.slot_end && slot >= p.slot_end[cnt * p.end_stride + j]) see = false;
+    }
+    float x = -INFINITY;
+    if (see) {
+      float d = 0.0f;
+      for (int e = 0; e < a.D; ++e) d += s_q[e] * load1((const T*)a.k_pages + at + e);
+      x = d * p.scale;
+    }
+    float mx = x;
+    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+    const float m2 = fmaxf(m, mx), base = m2 == -INFINITY ? 0.0f : m2;
+    const float pj = see ? expf(x - base) : 0.0f, al = expf(m - base);
+    float sum = pj;
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    l = l * al + sum;
+    m = m2;
+    for (int k = 0; k < 4; ++k) acc[k] *= al;
+    for (int jj = 0; jj < 64; ++jj) {
+      const float pv = __shfl(pj, jj, 64);
+      const int64_t av = __shfl(at, jj, 64);
+      if (!__shfl((int)see, jj, 64)) continue;
+      for (int k = 0; k * 64 + lane < a.D; ++k) acc[k] += pv * load1((const T*)a.v_pages + av + k * 64 + lane);
+    }
+  }
+  const bool none = l == 0.0f;
+  for (int k = 0; k * 64 + lane < a.D; ++k) {
+    const float o = none ? 0.0f : acc[k] / l;
+    T* dst = (T*)p.out + (t * a.Hq + h) * a.D + k * 64 + lane;
+    if constexpr (sizeof(T) == 2) dst->bits = __builtin_bit_cast(uint16_t, (__bf16)o);
+    else *dst = o;
+  }
+  if (lane == 0 && p.lse) p.lse[t * a.Hq + h] = none ? -INFINITY : m + logf(l);
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(int dtype, const KvArgs& a, const RotArgs& r, int32_t* status, hipStream_t s) {
+  prof_mark(KK_KV_APPEND, true, s);
+  const int chunks = a.D / (dtype == RLK_DTYPE_BF16 ? 8 : 4);
+  int lg = 0;
+  while ((1 << lg) < chunks) ++lg;
+  const int tpb = a.T >= 4096 ? kAppendTokens : 1;
+  const unsigned grid = (unsigned)((a.T + tpb - 1) / tpb) + 1;
+  if (dtype == RLK_DTYPE_BF16) k_kv_append<bf16_t><<<grid, 256, 0, s>>>(a, r, lg, tpb, status);
+  else k_kv_append<float><<<grid, 256, 0, s>>>(a, r, lg, tpb, status);
+  prof_mark(KK_KV_APPEND, false, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, int32_t* status, hipStream_t s) {
+  prof_mark(KK_KV_ATTENTION, true, s);
+  k_kv_check<<<1, 1024, 0, s>>>(a, status);
+  const dim3 grid((unsigned)a.T, (unsigned)a.Hq);
+  if (a.T > 0) {
+    if (dtype == RLK_DTYPE_BF16) k_kv_attention<bf16_t><<<grid, 64, 0, s>>>(a, p);
+    else k_kv_attention<float><<<grid, 64, 0, s>>>(a, p);
+  }
+  prof_mark(KK_KV_ATTENTION, false, s);
+  return hipGetLastError();
+}
+
+}  // namespace rlk

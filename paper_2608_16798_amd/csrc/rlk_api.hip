@@ -20,6 +20,9 @@ namespace rlk {
 static_assert(sizeof(rlk_batch_t) == 40, "rlk_batch_t layout");
 static_assert(sizeof(rlk_pg_params_t) == 80, "rlk_pg_params_t layout");
 static_assert(sizeof(rlk_pg_stats_t) == 64, "rlk_pg_stats_t layout");
+static_assert(sizeof(rlk_kv_t) == 88, "rlk_kv_t layout");
+static_assert(sizeof(rlk_rot_t) == 40, "rlk_rot_t layout");
+static_assert(sizeof(rlk_verify_t) == 40, "rlk_verify_t layout");
 
 namespace {
 
@@ -361,6 +364,97 @@ rlk_status_t finish(hipError_t e, const char* what, const void* ws, hipStream_t 
   return RLK_OK;
 }
 
+rlk_status_t check_kv(const rlk_kv_t* c) {
+  if (!c) return fail(RLK_EINVAL, "cache descriptor is NULL");
+  if (c->dtype != RLK_DTYPE_F32 && c->dtype != RLK_DTYPE_BF16) return fail(RLK_EDTYPE, "unknown dtype %d", c->dtype);
+  if (c->T < 0 || c->T >= ((int64_t)1 << 31)) return fail(RLK_ESHAPE, "T = %lld outside [0, 2^31)", (long long)c->T);
+  if (c->B < 0 || c->B > kMaxRollouts) return fail(RLK_ESHAPE, "B = %d outside [0, %d]", c->B, kMaxRollouts);
+  if (c->page_size < 1 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
+    return fail(RLK_ESHAPE, "page_size = %d must be a power of two in [1, 1024]", c->page_size);
+  if (c->n_pages < 0 || c->max_pages < 0) return fail(RLK_ESHAPE, "negative n_pages or max_pages");
+  if ((int64_t)c->max_pages * c->page_size >= ((int64_t)1 << 31))
+    return fail(RLK_ESHAPE, "max_pages * page_size = %lld exceeds the int32 slot",
+                (long long)c->max_pages * c->page_size);
+  if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8)
+    return fail(RLK_ESHAPE, "head_dim = %d must be a multiple of 8 in [8, 256]", c->head_dim);
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024)
+    return fail(RLK_ESHAPE, "n_kv_heads = %d outside [1, 1024]", c->n_kv_heads);
+  if (c->n_q_heads < c->n_kv_heads || c->n_q_heads % c->n_kv_heads || c->n_q_heads / c->n_kv_heads > 128 ||
+      c->n_q_heads > 16384)
+    return fail(RLK_ESHAPE, "n_q_heads = %d must be a multiple of n_kv_heads = %d, at most 128 to one and 16384 in all",
+                c->n_q_heads, c->n_kv_heads);
+  if (c->max_new < 0) return fail(RLK_EINVAL, "max_new must be >= 0");
+  if (c->reserved != 0) return fail(RLK_EINVAL, "reserved fields must be 0");
+  return RLK_OK;
+}
+
+// What the calls on a cache with rows need besides.
+rlk_status_t check_kv_pointers(const rlk_kv_t* c) {
+  if (!c->kv_len || !c->cu_new) return fail(RLK_EINVAL, "kv_len or cu_new is NULL");
+  if (c->max_pages > 0 && !c->page_table) return fail(RLK_EINVAL, "page_table is NULL");
+  if (c->n_pages > 0 && (!c->k_pages || !c->v_pages)) return fail(RLK_EINVAL, "k_pages or v_pages is NULL");
+  if (misaligned16(c->k_pages) || misaligned16(c->v_pages))
+    return fail(RLK_EINVAL, "k_pages and v_pages must be 16-byte aligned");
+  return RLK_OK;
+}
+
+rlk_status_t check_token_rows(const char* name, const void* p, int64_t stride, int64_t heads, int64_t dim) {
+  if (!p) return fail(RLK_EINVAL, "%s is NULL", name);
+  if (misaligned16(p)) return fail(RLK_EINVAL, "%s must be 16-byte aligned", name);
+  if (stride < heads * dim || stride % 8)
+    return fail(RLK_ESHAPE, "%s_stride = %lld must be a multiple of 8, at least %lld", name, (long long)stride,
+                (long long)(heads * dim));
+  return RLK_OK;
+}
+
+KvArgs kv_args(const rlk_kv_t* c) {
+  KvArgs a = {};
+  a.T = c->T;
+  a.B = c->B;
+  a.n_pages = c->n_pages;
+  while ((1 << a.ps_shift) < c->page_size) ++a.ps_shift;
+  a.max_pages = c->max_pages;
+  a.Hq = c->n_q_heads;
+  a.Hkv = c->n_kv_heads;
+  a.D = c->head_dim;
+  a.cap = (int64_t)c->max_pages * c->page_size;
+  a.k_pages = c->k_pages;
+  a.v_pages = c->v_pages;
+  a.table = c->page_table;
+  a.kv_len = c->kv_len;
+  a.cu = c->cu_new;
+  return a;
+}
+
+rlk_status_t check_verify(const rlk_verify_t* p) {
+  if (!p) return fail(RLK_EINVAL, "verify descriptor is NULL");
+  if (p->dtype != RLK_DTYPE_F32 && p->dtype != RLK_DTYPE_BF16) return fail(RLK_EDTYPE, "unknown dtype %d", p->dtype);
+  if (p->B < 0 || p->B > kMaxRollouts) return fail(RLK_ESHAPE, "B = %d outside [0, %d]", p->B, kMaxRollouts);
+  if (p->V < 1 || p->V > RLK_MAX_DIM) return fail(RLK_ESHAPE, "V = %d must lie in [1, %d]", p->V, RLK_MAX_DIM);
+  if (p->n_draft < 0) return fail(RLK_ESHAPE, "n_draft < 0");
+  if (p->B == 0 && p->n_draft != 0) return fail(RLK_ESHAPE, "B = 0 with n_draft = %lld", (long long)p->n_draft);
+  if (p->n_draft >= ((int64_t)1 << 30) || (2 * p->n_draft + p->B) * verify_chunks(p->V) >= ((int64_t)1 << 31))
+    return fail(RLK_ESHAPE, "n_draft = %lld rows of V = %d exceed one launch", (long long)p->n_draft, p->V);
+  if (p->temperature != 0.0f && !(p->temperature > 0.0f && isfinite(p->temperature)))
+    return fail(RLK_EINVAL, "temperature must be 0 (= 1) or finite and > 0");
+  return RLK_OK;
+}
+
+struct VerifyWs {
+  size_t hdr, part, mass, choice, total;
+};
+VerifyWs verify_layout(const rlk_verify_t* p) {
+  const int nc = verify_chunks(p->V);
+  Alloc a;
+  VerifyWs w;
+  w.hdr = a.take(sizeof(WsHeader));
+  w.part = a.take(verify_part_bytes(2 * p->n_draft + p->B, nc));
+  w.mass = a.take((size_t)p->B * nc * sizeof(double));
+  w.choice = a.take(verify_choice_bytes(p->B));
+  w.total = a.off;
+  return w;
+}
+
 #define RLK_TRY(expr, what)                      \
   do {                                           \
     hipError_t _e = (expr);                      \
@@ -401,7 +495,8 @@ const char* kKindNames[KK_COUNT_KINDS] = {
     "begin",        "compact_count", "compact_scan",  "compact_write", "rollout_offsets", "group_rank",
     "group_stats",  "advantage",     "transpose_w",   "gather",        "fwd_lse_gemm",    "lse_combine",
     "dz",           "dh_gemm",       "dw_gemm",       "loss_rollout",  "loss_final",      "zero_fill",
-    "gae",          "value_loss",    "value_head",    "target_logit",  "hidden_t"};
+    "gae",          "value_loss",    "value_head",    "target_logit",  "hidden_t",
+    "kv_append",    "kv_attention",  "draft_verify"};
 
 }  // namespace
 
@@ -1015,6 +1110,159 @@ rlk_status_t rlk_value_head_bwd(const rlk_batch_t* b, const void* hidden, const 
                                 dhidden, accumulate, dw_v, db_v, static_cast<char*>(ws), s),
           "value_head_bwd");
   return RLK_OK;
+}
+
+rlk_status_t rlk_kv_workspace_size(const rlk_kv_t* c, size_t* bytes) {
+  if (!bytes) return fail(RLK_EINVAL, "bytes is NULL");
+  rlk_status_t st = check_kv(c);
+  if (st) return st;
+  *bytes = align256(sizeof(WsHeader));
+  return RLK_OK;
+}
+
+rlk_status_t rlk_kv_append(const rlk_kv_t* c, const rlk_rot_t* r, const void* q, int64_t q_stride, const void* k,
+                           int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions, void* q_out,
+                           void* ws, size_t ws_bytes, void* stream) {
+  rlk_status_t st = check_kv(c);
+  if (st) return st;
+  if (!r) return fail(RLK_EINVAL, "rotation descriptor is NULL");
+  if (r->rot_style != RLK_ROT_HALF && r->rot_style != RLK_ROT_PAIRS)
+    return fail(RLK_EINVAL, "unknown rot_style %d", r->rot_style);
+  const int unit = r->rot_style == RLK_ROT_HALF ? 16 : 8;
+  if (r->rot_dim < 0 || r->rot_dim > c->head_dim || r->rot_dim % unit)
+    return fail(RLK_ESHAPE, "rot_dim = %d must be a multiple of %d in [0, head_dim = %d]", r->rot_dim, unit, c->head_dim);
+  if (r->rot_dim > 0 && !r->freq) return fail(RLK_EINVAL, "freq is NULL with rot_dim = %d", r->rot_dim);
+  if (!(r->norm_eps >= 0.0f && isfinite(r->norm_eps))) return fail(RLK_EINVAL, "norm_eps must be finite and >= 0");
+  if (r->reserved != 0) return fail(RLK_EINVAL, "reserved fields must be 0");
+  if (misaligned16(r->q_norm) || misaligned16(r->k_norm))
+    return fail(RLK_EINVAL, "q_norm and k_norm must be 16-byte aligned");
+  if (c->T > 0 && c->B > 0) {
+    st = check_kv_pointers(c);
+    if (!st) st = check_token_rows("k", k, k_stride, c->n_kv_heads, c->head_dim);
+    if (!st) st = check_token_rows("v", v, v_stride, c->n_kv_heads, c->head_dim);
+    if (!st && !q != !q_out) st = fail(RLK_EINVAL, "q and q_out come together");
+    if (!st && q) st = check_token_rows("q", q, q_stride, c->n_q_heads, c->head_dim);
+    if (!st && misaligned16(q_out)) st = fail(RLK_EINVAL, "q_out must be 16-byte aligned");
+    if (!st && q && q == q_out && q_stride != (int64_t)c->n_q_heads * c->head_dim)
+      st = fail(RLK_EINVAL, "q_out may be q only when q is contiguous");
+    if (st) return st;
+  }
+  st = check_ws(ws, ws_bytes, align256(sizeof(WsHeader)));
+  if (st) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  int32_t* status = &static_cast<WsHeader*>(ws)->status;
+  if (c->T == 0 || c->B == 0) {
+    RLK_TRY(launch_begin(static_cast<int32_t*>(ws), nullptr, 0, 0, s), "begin");
+    return finish(hipSuccess, "", ws, s);
+  }
+  RotArgs a = {};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out = q_out;
+  a.positions = positions;
+  a.freq = r->freq;
+  a.q_norm = q ? r->q_norm : nullptr;
+  a.k_norm = r->k_norm;
+  a.rot = r->rot_dim;
+  a.pairs = r->rot_style == RLK_ROT_PAIRS;
+  a.eps = r->norm_eps;
+  RLK_TRY(launch_kv_append(c->dtype, kv_args(c), a, status, s), "kv_append");
+  return finish(hipSuccess, "", ws, s);
+}
+
+rlk_status_t rlk_kv_attention(const rlk_kv_t* c, const void* q, int64_t q_stride, const int32_t* slot_end,
+                              int64_t end_stride, float scale, void* out, float* lse, void* ws, size_t ws_bytes,
+                              void* stream) {
+  rlk_status_t st = check_kv(c);
+  if (st) return st;
+  if (!isfinite(scale)) return fail(RLK_EINVAL, "scale must be finite");
+  if (slot_end && end_stride < 0) return fail(RLK_ESHAPE, "end_stride < 0");
+  if (c->T > 0 && c->B > 0) {
+    st = check_kv_pointers(c);
+    if (!st) st = check_token_rows("q", q, q_stride, c->n_q_heads, c->head_dim);
+    if (!st && !out) st = fail(RLK_EINVAL, "out is NULL");
+    if (!st && misaligned16(out)) st = fail(RLK_EINVAL, "out must be 16-byte aligned");
+    if (!st && out == q) st = fail(RLK_EINVAL, "out must not be q");
+    if (st) return st;
+  }
+  size_t need = 0;
+  st = rlk_kv_workspace_size(c, &need);
+  if (!st) st = check_ws(ws, ws_bytes, need);
+  if (st) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (c->T == 0 || c->B == 0) {
+    RLK_TRY(launch_begin(static_cast<int32_t*>(ws), nullptr, 0, 0, s), "begin");
+    return finish(hipSuccess, "", ws, s);
+  }
+  KvArgs k = kv_args(c);
+  if (slot_end) k.cap = std::min(k.cap, end_stride);  // a longer sequence would read past its row
+  AttnArgs a = {};
+  a.q = q;
+  a.q_stride = q_stride;
+  a.slot_end = slot_end;
+  a.end_stride = end_stride;
+  a.scale = scale;
+  a.out = out;
+  a.lse = lse;
+  RLK_TRY(launch_kv_attention(c->dtype, k, a, &static_cast<WsHeader*>(ws)->status, s), "kv_attention");
+  return finish(hipSuccess, "", ws, s);
+}
+
+rlk_status_t rlk_verify_workspace_size(const rlk_verify_t* p, size_t* bytes) {
+  if (!bytes) return fail(RLK_EINVAL, "bytes is NULL");
+  rlk_status_t st = check_verify(p);
+  if (st) return st;
+  *bytes = verify_layout(p).total;
+  return RLK_OK;
+}
+
+rlk_status_t rlk_draft_verify(const rlk_verify_t* p, const void* logits, const void* draft_logits, const int32_t* draft,
+                              const int32_t* cu_draft, const float* u_accept, const float* u_sample, int32_t* tokens,
+                              int32_t* n_accepted, float* logp, void* ws, size_t ws_bytes, void* stream) {
+  rlk_status_t st = check_verify(p);
+  if (st) return st;
+  if (p->ld_logits < p->V) return fail(RLK_ESHAPE, "ld_logits = %lld below V", (long long)p->ld_logits);
+  if (draft_logits && p->ld_draft < p->V) return fail(RLK_ESHAPE, "ld_draft = %lld below V", (long long)p->ld_draft);
+  if (p->B > 0 && (!logits || !cu_draft || !u_sample || !tokens || !n_accepted || !logp))
+    return fail(RLK_EINVAL, "logits, cu_draft, u_sample, tokens, n_accepted or logp is NULL");
+  if (p->n_draft > 0 && (!draft || !u_accept)) return fail(RLK_EINVAL, "draft or u_accept is NULL");
+  if (misaligned16(logits) || misaligned16(draft_logits))
+    return fail(RLK_EINVAL, "logits and draft_logits must be 16-byte aligned");
+  const VerifyWs L = verify_layout(p);
+  st = check_ws(ws, ws_bytes, L.total);
+  if (st) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  char* w = static_cast<char*>(ws);
+  if (p->B == 0) {
+    RLK_TRY(launch_begin(static_cast<int32_t*>(ws), nullptr, 0, 0, s), "begin");
+    return finish(hipSuccess, "", ws, s);
+  }
+  VerifyArgs a = {};
+  a.n_draft = p->n_draft;
+  a.ld_logits = p->ld_logits;
+  a.ld_draft = p->ld_draft;
+  a.B = p->B;
+  a.V = p->V;
+  a.nchunk = verify_chunks(p->V);
+  a.logits = logits;
+  a.draft_logits = p->n_draft > 0 ? draft_logits : nullptr;
+  a.draft = draft;
+  a.cu = cu_draft;
+  a.u_accept = u_accept;
+  a.u_sample = u_sample;
+  a.tokens = tokens;
+  a.n_accepted = n_accepted;
+  a.logp = logp;
+  a.inv_tau = p->temperature == 0.0f ? 1.0 : 1.0 / (double)p->temperature;
+  a.c = 1.4426950408889634 * a.inv_tau;
+  RLK_TRY(launch_draft_verify(p->dtype, a, w + L.part, reinterpret_cast<double*>(w + L.mass), w + L.choice,
+                              reinterpret_cast<int32_t*>(w + L.hdr), s),
+          "draft_verify");
+  return finish(hipSuccess, "", ws, s);
 }
 
 rlk_status_t rlk_check_status(const void* ws, void* stream, int32_t* flags) {

@@ -100,6 +100,9 @@ enum KernelKind {
   KK_VALUE_HEAD,
   KK_TARGET_LOGIT,
   KK_HIDDEN_T,
+  KK_KV_APPEND,
+  KK_KV_ATTENTION,
+  KK_VERIFY,
   KK_COUNT_KINDS
 };
 
@@ -273,6 +276,54 @@ hipError_t launch_value_head_fwd(int dtype, int64_t N, int d, int R, const void*
 hipError_t launch_value_head_bwd(int dtype, int64_t N, int d, int R, const void* h, const void* w,
                                  const uint8_t* mask, const int32_t* cu, const int32_t* gid, const float* dv,
                                  void* dh, int accumulate, float* dw, float* dbias, char* ws, hipStream_t s);
+
+// ---- launchers (k_kv.hip) ----
+struct KvArgs {
+  int64_t T;
+  int B, n_pages, ps_shift, max_pages, Hq, Hkv, D;  // page size 2^ps_shift
+  int64_t cap;                                      // slots of a page-table row
+  void *k_pages, *v_pages;
+  const int32_t *table, *kv_len, *cu;
+};
+struct RotArgs {
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  void* q_out;
+  const int32_t* positions;  // NULL: the slot
+  const double* freq;
+  const void *q_norm, *k_norm;
+  int rot;
+  bool pairs;
+  float eps;
+};
+hipError_t launch_kv_append(int dtype, const KvArgs& a, const RotArgs& r, int32_t* status, hipStream_t s);
+struct AttnArgs {
+  const void* q;
+  int64_t q_stride;
+  const int32_t* slot_end;  // NULL: causal only
+  int64_t end_stride;
+  float scale;
+  void* out;
+  float* lse;  // may be NULL
+};
+hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, int32_t* status, hipStream_t s);
+
+// ---- launchers (k_verify.hip) ----
+struct VerifyArgs {
+  int64_t n_draft, ld_logits, ld_draft;
+  int B, V, nchunk;
+  const void *logits, *draft_logits;
+  const int32_t *draft, *cu;
+  const float *u_accept, *u_sample;
+  int32_t *tokens, *n_accepted;
+  float* logp;
+  double c, inv_tau;  // log2(e) / tau, 1 / tau
+};
+int verify_chunks(int V);
+size_t verify_part_bytes(int64_t rows, int nchunk);
+size_t verify_choice_bytes(int B);
+hipError_t launch_draft_verify(int dtype, const VerifyArgs& a, void* part, double* mass, void* choice, int32_t* status,
+                               hipStream_t s);
 
 // ---- launchers (k_gemm.hip) ----
 struct GemmArgs {

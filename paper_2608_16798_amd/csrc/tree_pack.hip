@@ -211,3 +211,36 @@ extern "C" rlk_status_t rlk_tree_pack(const rlk_calls_t* calls, rlk_tree_out_t* 
   }
   return RLK_OK;
 }
+
+extern "C" rlk_status_t rlk_tree_ends(int32_t R, const int64_t* pos_off, const int32_t* parent, int32_t* end) {
+  if (R < 0) return report_error(RLK_ESHAPE, "R < 0");
+  if (R == 0) return RLK_OK;
+  if (!pos_off) return report_error(RLK_EINVAL, "pos_off is NULL");
+  if (pos_off[0] != 0) return report_error(RLK_EINVAL, "pos_off[0] must be 0");
+  for (int r = 0; r < R; ++r)
+    if (pos_off[r + 1] < pos_off[r]) return report_error(RLK_EINVAL, "pos_off decreases");
+  if (pos_off[R] > INT32_MAX) return report_error(RLK_ESHAPE, "more than 2^31 packed positions");
+  if (pos_off[R] > 0 && (!parent || !end)) return report_error(RLK_EINVAL, "parent or end is NULL");
+  try {
+    std::vector<int32_t> path;  // the positions from the root to the one before
+    for (int r = 0; r < R; ++r) {
+      const int64_t o = pos_off[r], n = pos_off[r + 1] - o;
+      path.clear();
+      for (int64_t i = 0; i <= n; ++i) {
+        const int64_t up = i < n && parent[o + i] >= 0 ? parent[o + i] - o : -1;  // local; -1 behind the last position
+        if (i < n && (parent[o + i] < -1 || (parent[o + i] >= 0 && (up < 0 || up >= i))))
+          return report_error(RLK_EINVAL, "a parent lies outside its rollout or not before its position");
+        // what the next position does not descend from is complete
+        while (!path.empty() && path.back() != up) {
+          end[o + path.back()] = (int32_t)i;
+          path.pop_back();
+        }
+        if (up >= 0 && path.empty()) return report_error(RLK_EINVAL, "the positions are not in depth-first order");
+        if (i < n) path.push_back((int32_t)i);
+      }
+    }
+  } catch (const std::bad_alloc&) {
+    return report_error(RLK_ESHAPE, "out of host memory");
+  }
+  return RLK_OK;
+}

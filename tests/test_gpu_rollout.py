@@ -1,0 +1,717 @@
+"""Rollout side on the GPU against the fp64 oracle: append to the paged cache, attention of the new tokens over it,
+verification of drafted tokens, and the three run together in front of the loss.
+
+Tolerances count roundings: half a step is U = 2^-8 (bf16) or 2^-24 (fp32) of the value.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_16798_amd as rlk
+from gpu_common import ensure_library, log, to_host
+from oracle import rollout as RO
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+U = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+E = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    ensure_library()
+
+
+def dev(a, dtype=torch.int32):
+    return torch.as_tensor(np.ascontiguousarray(a), device="cuda").to(dtype)
+
+
+def host(t):
+    return to_host(t).astype(np.float64)
+
+
+def build(seqs, K, ps, D, dtype, seed, extra_cols=2, fill=float("nan")):
+    """A cache for sequences of (cached, new) tokens: pages in no order, what no slot below kv_len uses holds `fill`."""
+    rng = np.random.default_rng(seed)
+    lens = np.array([c + n for c, n in seqs], np.int64)
+    used = -(-lens // ps)
+    pool = int(used.sum()) + 3
+    table = rng.integers(-5, pool + 5, (len(seqs), max(1, int(used.max(initial=0))) + extra_cols))  # junk behind the last page
+    pages = rng.permutation(pool)
+    at = 0
+    for b, u in enumerate(used):
+        table[b, :u] = pages[at:at + u]
+        at += u
+    k, v = (torch.full((pool, K, ps, D), fill, dtype=DT[dtype], device="cuda") for _ in range(2))
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    for b, n in enumerate(lens):
+        if n:
+            j = np.arange(n)
+            pg, sl = dev(table[b, j // ps], torch.int64), dev(j % ps, torch.int64)
+            k[pg, :, sl] = torch.randn(n, K, D, generator=gen, device="cuda").to(DT[dtype])
+            v[pg, :, sl] = torch.randn(n, K, D, generator=gen, device="cuda").to(DT[dtype])
+    cu = np.concatenate([[0], np.cumsum([n for _, n in seqs])]).astype(np.int64)
+    return dict(k_pages=k, v_pages=v, page_table=dev(table), kv_len=dev(lens), cu_new=dev(cu)), table, lens, cu, gen
+
+
+# ---- append ----
+
+APPEND = [
+    # seqs (cached, new), Hq, Hkv, D, page, rot, style, norm, dtype
+    ([(0, 1)], 4, 2, 128, 16, 128, "half", True, "bf16"),
+    ([(5, 1), (0, 3), (63, 2), (16, 0), (0, 0), (1, 16)], 8, 2, 64, 16, 64, "half", True, "bf16"),
+    ([(5, 7), (100, 33)], 10, 2, 80, 8, 40, "pairs", False, "f32"),
+    ([(5, 7), (100, 33)], 10, 2, 80, 8, 48, "half", True, "f32"),
+    ([(3, 9)], 3, 1, 8, 1, 8, "pairs", True, "f32"),
+    ([(3, 9)], 3, 1, 8, 1, 0, "half", True, "bf16"),
+    ([(1000, 5), (7, 1)], 5, 5, 256, 1024, 256, "half", False, "f32"),
+    ([(1000, 5), (7, 1)], 7, 1, 200, 2, 96, "half", True, "bf16"),
+    ([(9, 2500), (0, 2000)], 6, 2, 72, 32, 72, "pairs", True, "bf16"),
+]
+
+
+@pytest.mark.parametrize("seqs,H,K,D,ps,rot,style,norm,dtype", APPEND)
+@pytest.mark.parametrize("given", [False, True], ids=["slots", "positions"])
+def test_append(seqs, H, K, D, ps, rot, style, norm, dtype, given):
+    log(f"append {seqs} H={H} K={K} D={D} page={ps} rot={rot} {style} norm={norm} {dtype} positions={given}")
+    c, table, lens, cu, gen = build(seqs, K, ps, D, dtype, seed=D + ps, fill=0.5)
+    T = int(cu[-1])
+    qkv = torch.randn(T + 2, H + 2 * K, D, generator=gen, device="cuda").to(DT[dtype])  # two rows behind the last sequence
+    q, k, v = qkv[:, :H], qkv[:, H:H + K], qkv[:, H + K:]
+    w = [torch.randn(D, generator=gen, device="cuda").to(DT[dtype]) for _ in range(2)] if norm else [None, None]
+    freq = None if rot == 0 else 1e4 ** (-torch.arange(0, rot, 2, dtype=torch.float64, device="cuda") / rot)
+    pos = None
+    if given:
+        pos = torch.randint(-1000, 1 << 22, (T + 2,), generator=gen, device="cuda", dtype=torch.int32)
+    before = [host(c["k_pages"]), host(c["v_pages"])]
+    q_out = torch.full((T + 2, H, D), 7.0, dtype=DT[dtype], device="cuda")
+    got, ws = rlk.kv_append(**c, q=q, k=k, v=v, freq=freq, positions=pos, q_norm=w[0], k_norm=w[1], norm_eps=1e-5,
+                            rot_style=style, q_out=q_out)
+    assert rlk.check_status(ws) == 0
+    opt = lambda t: None if t is None else host(t)  # noqa: E731
+    ref = RO.kv_append(before[0], before[1], table, lens, cu, host(q), host(k), host(v), opt(freq), opt(pos), opt(w[0]),
+                       opt(w[1]), 1e-5, style)
+    # the norm's sum of D squares, its root and the product (D / 2 + 4), sine, cosine, two products and a sum (8)
+    rel = (D / 2 + 12) * E
+    for name, a, r, mag, rows in (("q", got, ref["q"], ref["q_mag"], T), ("k", c["k_pages"], ref["k_pages"], ref["k_mag"], None)):
+        d = np.abs(host(a) - r)[:rows]
+        lim = (U[dtype] * np.abs(r) + rel * mag)[:rows]
+        assert np.all(d <= lim), (name, float((d - lim).max()))
+    np.testing.assert_array_equal(host(c["v_pages"]), ref["v_pages"])
+    assert bool((got[T:] == 7.0).all())
+    # keys and values alone, and the queries in place
+    c2 = dict(c, k_pages=torch.full_like(c["k_pages"], 0.5), v_pages=torch.full_like(c["v_pages"], 0.5))
+    rlk.kv_append(**c2, q=None, k=k, v=v, freq=freq, positions=pos, k_norm=w[1], norm_eps=1e-5, rot_style=style, ws=ws)
+    own = torch.zeros_like(c["k_pages"], dtype=torch.bool)
+    for b, slot in RO.slots(lens, cu):
+        own[int(table[b, slot // ps]), :, slot % ps] = True
+    assert torch.equal(c2["k_pages"][own], c["k_pages"][own]) and torch.equal(c2["v_pages"][own], c["v_pages"][own])
+    assert bool((c2["k_pages"][~own] == 0.5).all()) and bool((c2["v_pages"][~own] == 0.5).all())
+    qc = q.contiguous()
+    rlk.kv_append(**c2, q=qc, k=k, v=v, freq=freq, positions=pos, q_norm=w[0], k_norm=w[1], norm_eps=1e-5, rot_style=style,
+                  q_out=qc, ws=ws)
+    assert torch.equal(qc[:T], got[:T])
+
+
+def test_append_far_positions():
+    """Angles of 2 billion: whole turns come off before fp32."""
+    c, table, lens, cu, gen = build([(0, 3)], 1, 16, 64, "f32", 1)
+    x = torch.randn(3, 1, 64, generator=gen, device="cuda")
+    freq = 1e4 ** (-torch.arange(0, 64, 2, dtype=torch.float64, device="cuda") / 64)
+    pos = dev([2 ** 31 - 1, -2 ** 31, 123456789])
+    got, _ = rlk.kv_append(**c, q=x, k=x, v=x, freq=freq, positions=pos)
+    for t in range(3):
+        ang = int(pos[t]) * host(freq)
+        ref, mag = RO._rotate(host(x)[t], ang, "half")
+        # a turn count of 3.4e8 rounds by 2^-25 of a turn in fp64 twice (product, 1 / 2 pi), 2e-7 radians each
+        assert np.all(np.abs(host(got)[t] - ref) <= (16 * E + 5e-7) * mag)
+
+
+# ---- attention ----
+
+def score_error(ref, D):
+    """Error of a score in fp32: D products and sums, the scale, the argument of the exponential (6 roundings of |x|)."""
+    return (D + 4) * E * ref["mag"] + 6 * E * ref["top"]
+
+
+def check_attention(c, table, lens, cu, q, dtype, scale, ends=None, max_new=0, out=None, kv=None, tag=""):
+    T, H, D = q.shape
+    if out is None:
+        out = torch.full((T, H, D), 7.0, dtype=DT[dtype], device="cuda")
+    lse = torch.full((T, H), 7.0, dtype=torch.float32, device="cuda")
+    got, _, ws = rlk.kv_attention(q, **c, scale=scale, slot_end=None if ends is None else dev(ends), max_new=max_new, out=out,
+                                  lse=lse)
+    assert rlk.check_status(ws) == 0
+    kp, vp = kv or (host(c["k_pages"]), host(c["v_pages"]))
+    with np.errstate(invalid="ignore"):
+        ref = RO.kv_attention(host(q), kp, vp, table, lens, cu, scale, ends)
+    n = int(cu[-1])
+    o, l = host(got), host(lse)
+    assert np.all(o[n:] == 7.0) and np.all(l[n:] == 7.0)
+    empty = np.isneginf(ref["lse"][:n])
+    assert np.array_equal(np.isneginf(l[:n]), empty) and np.all(o[:n][empty] == 0.0)
+    x = score_error(ref, D)[:n]
+    keys = 1 + max(int(v) for v in lens) if len(lens) else 1
+    # weights: twice the score's error (its own and the largest's), a rounding to the dtype for the product, the
+    # sums over the keys (numerator and denominator), exponential, rescaling and quotient (2^-20)
+    rel = U[dtype] + 2 * x + 2 * keys * E + 2.0 ** -20
+    lim = rel[..., None] * ref["pv"][:n] + U[dtype] * np.abs(ref["out"][:n])
+    d = np.abs(o[:n] - ref["out"][:n])
+    with np.errstate(invalid="ignore"):
+        worst = float(np.nanmax(d / np.maximum(lim, 1e-30))) if d.size else 0.0
+    log(f"  {tag} out {worst:.3f} of the bound")
+    assert np.all(d <= lim), (tag, worst)
+    dl = np.abs(l[:n][~empty] - ref["lse"][:n][~empty])
+    ll = (x + keys * E + 2.0 ** -20 + 2 * E * np.abs(np.where(empty, 0.0, ref["lse"][:n])))[~empty]
+    assert np.all(dl <= ll), (tag, float((dl - ll).max()))
+    return got, lse, ws
+
+
+ATTEND = [
+    # seqs (cached, new), Hq, Hkv, D, page, dtype
+    ([(0, 1)], 1, 1, 128, 16, "bf16"),
+    ([(0, 1)], 4, 1, 8, 1, "f32"),
+    ([(31, 1), (32, 1), (33, 1), (63, 1), (64, 1), (127, 1), (128, 1), (129, 1), (0, 1)], 8, 2, 128, 16, "bf16"),
+    ([(300, 1), (0, 0), (17, 2), (0, 5), (1200, 4)], 8, 2, 64, 8, "bf16"),
+    ([(300, 1), (0, 0), (17, 2), (0, 5), (700, 4)], 10, 2, 80, 16, "f32"),
+    ([(0, 33), (1, 32), (77, 31), (200, 64), (0, 65)], 4, 2, 128, 64, "bf16"),
+    ([(0, 130), (50, 200), (3, 1)], 7, 1, 128, 32, "bf16"),
+    ([(0, 130), (50, 77), (3, 1)], 5, 1, 96, 32, "f32"),
+    ([(10, 3), (500, 20)], 40, 1, 64, 128, "bf16"),
+    ([(10, 3), (60, 4)], 128, 1, 64, 2, "bf16"),
+    ([(10, 3), (300, 40)], 6, 6, 256, 16, "bf16"),
+    ([(10, 3), (300, 40)], 3, 3, 256, 1024, "f32"),
+    ([(100, 9), (0, 150)], 4, 2, 200, 16, "bf16"),
+    ([(100, 9), (0, 40)], 4, 2, 24, 4, "bf16"),
+    ([(2100, 1)], 2, 1, 128, 1, "bf16"),
+    ([(3, 2)] * 70, 2, 1, 64, 16, "bf16"),
+]
+
+
+@pytest.mark.parametrize("seqs,H,K,D,ps,dtype", ATTEND)
+def test_attention(seqs, H, K, D, ps, dtype):
+    log(f"attention {seqs[:9]} H={H} K={K} D={D} page={ps} {dtype}")
+    c, table, lens, cu, gen = build(seqs, K, ps, D, dtype, seed=H + D)
+    T = int(cu[-1])
+    wide = torch.randn(T + 3, H + 1, D, generator=gen, device="cuda").to(DT[dtype])
+    q = wide[:, :H]  # strided rows, three of them behind the last sequence
+    first = check_attention(c, table, lens, cu, q, dtype, 1.2 / math.sqrt(D), tag="causal")
+    # the hint plans tiles only; a call repeats itself bit for bit
+    again = check_attention(c, table, lens, cu, q, dtype, 1.2 / math.sqrt(D), tag="again")
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    for hint in (1, 40, 1 << 20):
+        check_attention(c, table, lens, cu, q, dtype, 1.2 / math.sqrt(D), max_new=hint, tag=f"hint {hint}")
+
+
+@pytest.mark.parametrize("seqs,H,K,D,ps,dtype", [ATTEND[i] for i in (2, 3, 4, 5, 6, 7, 8, 10, 11, 12)])
+def test_attention_of_trees(seqs, H, K, D, ps, dtype):
+    """Random trees over every sequence, some positions seen by nobody, some tokens that see nothing."""
+    log(f"tree attention {seqs[:9]} H={H} K={K} D={D} page={ps} {dtype}")
+    c, table, lens, cu, gen = build(seqs, K, ps, D, dtype, seed=H + D + 1)
+    rng = np.random.default_rng(D)
+    ends = np.full((len(seqs), int(lens.max()) + 5), -3, np.int64)
+    for b, n in enumerate(lens):
+        parent = [-1] + [int(rng.choice([i - 1, i - 1, i - 1, max(0, i - 1 - int(rng.integers(0, 9)))])) for i in range(1, n)]
+        for i in range(1, n):  # make it depth first: a parent on the path of the one before
+            path, j = [], i - 1
+            while j >= 0:
+                path.append(j)
+                j = parent[j]
+            parent[i] = max(p for p in path if p <= parent[i]) if parent[i] >= 0 else -1
+        ends[b, :n] = rlk.tree_ends([0, n], parent[:n])
+    ends[:, 0] = np.where(rng.random(len(seqs)) < 0.5, 0, ends[:, 0])  # the first slot sees not even itself
+    ends[-1, :lens[-1]] = np.minimum(ends[-1, :lens[-1]], lens[-1] - 1)  # the last token of the last sequence sees nothing
+    q = torch.randn(int(cu[-1]), H, D, generator=gen, device="cuda").to(DT[dtype])
+    check_attention(c, table, lens, cu, q, dtype, 1.0 / math.sqrt(D), ends=ends, tag="tree")
+    check_attention(c, table, lens, cu, q, dtype, 1.0 / math.sqrt(D), ends=np.zeros_like(ends), tag="nothing to see")
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dtype,new,D", [("bf16", 5, 128), ("bf16", 90, 64), ("bf16", 90, 256), ("f32", 5, 80), ("f32", 90, 128)])
+def test_unseen_keys_and_values_stay_out(dtype, new, D, bad):
+    """Keys and values of slots that a token does not see (later ones, another branch) are anything at all."""
+    log(f"unseen {bad} {dtype} new={new} D={D}")
+    c, table, lens, cu, gen = build([(70, new)], 2, 16, D, dtype, seed=new)
+    n = 70 + new
+    ends = np.full((1, n), n, np.int64)
+    ends[0, 40:60] = 60           # a finished branch: no new token sees it
+    ends[0, 71] = 72              # a leaf: only its own token sees it
+    q = torch.randn(new, 4, D, generator=gen, device="cuda").to(DT[dtype])
+    clean = (c["k_pages"].clone(), c["v_pages"].clone())
+    for slot in (41, 55, 59, 71, n - 1):
+        pg, sl = int(table[0, slot // 16]), slot % 16
+        c["k_pages"][pg, :, sl] = bad
+        c["v_pages"][pg, :, sl, ::3] = bad
+    out, lse, _ = rlk.kv_attention(q, **c, scale=0.2, slot_end=dev(ends), lse=torch.empty(new, 4, device="cuda"))
+    cc = dict(c, k_pages=clean[0], v_pages=clean[1])
+    ref, rl, _ = rlk.kv_attention(q, **cc, scale=0.2, slot_end=dev(ends), lse=torch.empty(new, 4, device="cuda"))
+    see = np.array([70 + i in (71, n - 1) for i in range(new)])
+    keep = dev(np.flatnonzero(~see), torch.int64)
+    assert torch.equal(out[keep], ref[keep]) and torch.equal(lse[keep], rl[keep])
+    assert bool(torch.isfinite(out[keep]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [2, 80])
+def test_extreme_scores(dtype, new):
+    """Scores of thousands (one key takes all), equal scores, and a scale of zero (the mean)."""
+    c, table, lens, cu, gen = build([(150, new)], 1, 16, 128, dtype, seed=9)
+    q = torch.randn(new, 2, 128, generator=gen, device="cuda").to(DT[dtype])
+    for scale in (30.0, -30.0, 0.0, 1e-20):
+        # a score of 2,000 in fp32 is off by 1e-3 to 1e-2: the bound follows it
+        check_attention(c, table, lens, cu, q, dtype, scale, tag=f"scale {scale}")
+    c["k_pages"].zero_()
+    check_attention(c, table, lens, cu, q, dtype, 1.0, kv=(np.zeros(c["k_pages"].shape), host(c["v_pages"])), tag="equal")
+
+
+def test_shared_prefix_pages():
+    """Rollouts of one task share the prompt's pages."""
+    c, table, lens, cu, gen = build([(200, 3), (220, 1), (200, 70)], 2, 16, 64, "bf16", seed=2)
+    table = table.copy()
+    table[1, :12] = table[0, :12]
+    table[2, :12] = table[0, :12]
+    c["page_table"] = dev(table)
+    q = torch.randn(int(cu[-1]), 4, 64, generator=gen, device="cuda").to(torch.bfloat16)
+    check_attention(c, table, lens, cu, q, "bf16", 0.125, tag="shared")
+
+
+@pytest.mark.parametrize("new", [2, 70])
+def test_pool_past_32_bits(new):
+    """A pool of more than 2^31 elements (and 2^32 bytes): the sequence lies in its last pages."""
+    K, ps, D = 2, 64, 128
+    n_pages = (1 << 31) // (K * ps * D) + 40
+    k, v = (torch.empty(n_pages, K, ps, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert k.numel() > 1 << 31
+    n = 300 + new
+    table = np.arange(n_pages - 6, n_pages)[None, ::-1].copy()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for p in range(n_pages - 6, n_pages):
+        k[p], v[p] = (torch.randn(K, ps, D, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    c = dict(k_pages=k, v_pages=v, page_table=dev(table), kv_len=dev([n]), cu_new=dev([0, new]))
+    q, kn, vn = (torch.randn(new, h, D, generator=gen, device="cuda").to(torch.bfloat16) for h in (4, K, K))
+    _, ws = rlk.kv_append(**c, q=q, k=kn, v=vn)
+    assert rlk.check_status(ws) == 0
+    j = np.arange(300, n)
+    pg, sl = dev(table[0, j // ps], torch.int64), dev(j % ps, torch.int64)
+    assert torch.equal(k[pg, :, sl], kn) and torch.equal(v[pg, :, sl], vn)
+    small = (k[-6:].clone(), v[-6:].clone())
+    lse = torch.empty(new, 4, device="cuda")
+    out, _, ws = rlk.kv_attention(q, **c, lse=lse)
+    ref = RO.kv_attention(host(q), host(small[0]), host(small[1]), table - (n_pages - 6), [n], [0, new], D ** -0.5)
+    assert rlk.check_status(ws) == 0
+    lim = (2.0 ** -8 + 2 * score_error(ref, D) + 2 * n * E + 2.0 ** -20)[..., None] * ref["pv"] + 2.0 ** -8 * np.abs(ref["out"])
+    assert np.all(np.abs(host(out) - ref["out"]) <= lim)
+
+
+def test_bad_device_data_is_reported_and_stays_in_bounds():
+    def fresh():
+        return build([(20, 2), (5, 3), (0, 40)], 2, 8, 64, "bf16", 4)
+
+    c, table, lens, cu, gen = fresh()
+    T = int(cu[-1])
+    q, k, v = (torch.randn(T, h, 64, generator=gen, device="cuda").to(torch.bfloat16) for h in (4, 2, 2))
+    good, _, _ = rlk.kv_attention(q, **c)
+
+    def both(want_append, want_attend, rows=None, **over):
+        c2 = dict(fresh()[0], **over)
+        out = torch.full_like(q, 7.0)
+        q_out = torch.full_like(q, 7.0)
+        _, _, ws = rlk.kv_attention(q, **c2, out=out)
+        assert rlk.check_status(ws) == want_attend
+        _, ws = rlk.kv_append(**c2, q=q, k=k, v=v, q_out=q_out, ws=ws)
+        assert rlk.check_status(ws) == want_append
+        if rows is not None:
+            assert bool((out[rows] == 7.0).all()) and bool((q_out[rows] == 7.0).all())
+            keep = [r for r in range(T) if r not in rows]
+            assert torch.equal(out[keep], good[keep])
+
+    both(0, 0)
+    both(rlk.DERR_KV_LEN, rlk.DERR_KV_LEN, rows=[2, 3, 4], kv_len=dev([22, 2, 40]))       # fewer than the new tokens
+    both(rlk.DERR_KV_LEN, rlk.DERR_KV_LEN, rows=[2, 3, 4], kv_len=dev([22, 10 ** 6, 40]))
+    both(rlk.DERR_KV_LEN, rlk.DERR_KV_LEN, rows=[0, 1], kv_len=dev([-4, 8, 40]))
+    both(rlk.DERR_CU_SEQLENS, rlk.DERR_CU_SEQLENS, cu_new=dev([1, 2, 5, T]))
+    both(rlk.DERR_CU_SEQLENS, rlk.DERR_CU_SEQLENS, rows=list(range(5, T)), cu_new=dev([0, 2, 5, T + 1]))
+    t2 = table.copy()
+    t2[0, 0] = 10 ** 6   # a page of the history: only the attention reads it
+    both(0, rlk.DERR_PAGE, page_table=dev(t2))
+    t2[0, 2] = -1        # the page that takes the new tokens
+    both(rlk.DERR_PAGE, rlk.DERR_PAGE, page_table=dev(t2))
+    # a row of slot_end shorter than the sequence
+    out = torch.full_like(q, 7.0)
+    _, _, ws = rlk.kv_attention(q, **c, slot_end=torch.full((3, 30), 1000, dtype=torch.int32, device="cuda"), out=out)
+    assert rlk.check_status(ws) == rlk.DERR_KV_LEN
+    assert bool((out[5:] == 7.0).all()) and torch.equal(out[:5], good[:5])
+    _, _, ws = rlk.kv_attention(q, **c, ws=ws)
+    assert rlk.check_status(ws) == 0  # the next call on the workspace starts afresh
+
+
+def test_no_tokens():
+    c, *_ = build([(4, 0), (0, 0)], 2, 8, 64, "bf16", 4)
+    q, k = (torch.empty(0, h, 64, dtype=torch.bfloat16, device="cuda") for h in (4, 2))
+    out, lse, ws = rlk.kv_attention(q, **c, lse=torch.empty(0, 4, device="cuda"))
+    assert out.shape == (0, 4, 64) and rlk.check_status(ws) == 0
+    q_out, ws = rlk.kv_append(**c, q=q, k=k, v=k)
+    assert q_out.shape == (0, 4, 64) and rlk.check_status(ws) == 0
+    none = dict(k_pages=c["k_pages"], v_pages=c["v_pages"], page_table=torch.empty(0, 4, dtype=torch.int32, device="cuda"),
+                kv_len=torch.empty(0, dtype=torch.int32, device="cuda"), cu_new=torch.zeros(1, dtype=torch.int32, device="cuda"))
+    rows = torch.full((3, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    out, _, ws = rlk.kv_attention(torch.zeros_like(rows), **none, out=rows)
+    assert rlk.check_status(ws) == 0 and bool((out == 7.0).all())
+
+
+# ---- verification ----
+
+def verify_inputs(n, V, dtype, dist, seed, tau):
+    rng = np.random.default_rng(seed)
+    n = np.asarray(n)
+    B, cu = len(n), np.concatenate([[0], np.cumsum(n)])
+    nd, rows = int(cu[-1]), int(cu[-1]) + B
+    z = rng.standard_normal((rows, V)) * 1.5
+    likely = rng.integers(0, V, rows)
+    z[np.arange(rows), likely] += rng.uniform(2, 14, rows) * tau
+    at = np.concatenate([cu[b] + b + np.arange(n[b]) for b in range(B)]).astype(int) if nd else np.zeros(0, int)
+    draft = np.where(rng.random(nd) < 0.7, likely[at], rng.integers(0, V, nd))
+    zq = z[at] + 0.8 * rng.standard_normal((nd, V)) if dist else None
+    t = lambda a: None if a is None else torch.as_tensor(a, device="cuda").to(DT[dtype])  # noqa: E731
+    return dict(logits=t(z), draft=dev(draft), cu_draft=dev(cu), u_accept=dev(rng.random(nd), torch.float32),
+                u_sample=dev(rng.random(B), torch.float32), draft_logits=t(zq), temperature=tau)
+
+
+def oracle_verify(a):
+    g = lambda t: None if t is None else host(t)  # noqa: E731
+    return RO.draft_verify(g(a["logits"]), a["draft"].cpu().numpy(), a["cu_draft"].cpu().numpy(), host(a["u_accept"]),
+                           host(a["u_sample"]), g(a["draft_logits"]), float(np.float32(a["temperature"])))
+
+
+def check_verify(a, tag, status=0):
+    tok, acc, logp, ws = rlk.draft_verify(**a)
+    assert rlk.check_status(ws) == status
+    ref = oracle_verify(a)
+    np.testing.assert_array_equal(acc.cpu().numpy(), ref["n_accepted"], err_msg=tag)
+    np.testing.assert_array_equal(tok.cpu().numpy(), ref["tokens"], err_msg=tag)
+    # fp64 up to the one rounding
+    assert np.all(np.abs(host(logp) - ref["logp"]) <= 1.01 * E * np.abs(ref["logp"]) + 1e-10), tag
+    return ref
+
+
+VERIFY = [
+    # drafts per sequence, V, dtype, temperature
+    ([0], 1, "f32", 1.0), ([3], 2, "bf16", 1.0), ([4], 50, "f32", 0.7), ([0, 1, 2, 3, 4, 5, 6, 7, 8, 9], 300, "bf16", 1.3),
+    ([4, 4], 4095, "f32", 1.0), ([4, 4], 4096, "bf16", 1.0), ([4, 0, 4], 4097, "f32", 0.5), ([2, 0, 5, 1], 50021, "bf16", 1.0),
+    ([2, 0, 5, 1], 50021, "f32", 0.8), ([1] * 40, 1001, "bf16", 1.0), ([70, 33], 700, "f32", 1.0), ([4] * 6, 151936, "bf16", 1.0),
+]
+
+
+@pytest.mark.parametrize("n,V,dtype,tau", VERIFY)
+@pytest.mark.parametrize("dist", [True, False], ids=["draft_logits", "tokens_only"])
+def test_verify(n, V, dtype, tau, dist):
+    log(f"verify n={n[:10]} V={V} {dtype} tau={tau} dist={dist}")
+    for seed in range(3):
+        ref = check_verify(verify_inputs(n, V, dtype, dist, 100 * seed + V, tau), f"seed {seed}")
+        log(f"  accepted {ref['n_accepted'][:10]}")
+
+
+def test_verify_edges():
+    log("verify edges")
+    a = verify_inputs([4, 4, 2], 5000, "f32", True, 1, 1.0)
+    check_verify(dict(a, u_accept=torch.zeros_like(a["u_accept"])), "u_accept 0: everything with mass is accepted")
+    check_verify(dict(a, u_accept=torch.full_like(a["u_accept"], 1 - E)), "u_accept at its top")
+    check_verify(dict(a, u_sample=torch.zeros_like(a["u_sample"])), "u_sample 0: the lowest token with mass")
+    check_verify(dict(a, u_sample=torch.full_like(a["u_sample"], 1 - E)), "u_sample at its top")
+    # the draft model agrees with the target bit for bit: all accepted whatever u
+    at = dev([0, 1, 2, 3, 5, 6, 7, 8, 10, 11], torch.int64)
+    same = dict(a, draft_logits=a["logits"][at].clone(), u_accept=torch.full_like(a["u_accept"], 1 - E))
+    assert check_verify(same, "q = p")["n_accepted"].tolist() == [4, 4, 2]
+    # masked vocabularies: whole chunks of -inf, a draft without mass, one token left
+    m = dict(a, logits=a["logits"].clone(), draft_logits=a["draft_logits"].clone(), draft=a["draft"].clone())
+    m["logits"][:, :4500] = -math.inf
+    m["logits"][3, :] = -math.inf
+    m["logits"][3, 4999] = -50.0
+    m["draft_logits"][:, 100:] = -math.inf
+    m["draft"][:] = 7
+    check_verify(m, "masked")
+    m2 = dict(m, draft_logits=None)
+    check_verify(m2, "masked, tokens only")
+    # far logits: sums span hundreds of powers of two
+    f = dict(a, logits=a["logits"] * 300, draft_logits=a["draft_logits"] * 300)
+    check_verify(f, "far logits")
+    check_verify(dict(f, temperature=300.0), "far logits, high temperature")
+
+
+def test_verify_random_numbers_of_one_and_rows_behind_the_last():
+    a = verify_inputs([2, 3], 300, "f32", True, 5, 1.0)
+    out = dict(tokens=dev(np.full(7, 77)), logp=torch.full((7,), 7.0, device="cuda"))
+    # u of 1 lies outside [0, 1): still a token with mass
+    tok, acc, logp, ws = rlk.draft_verify(**dict(a, u_sample=torch.ones(2, device="cuda")), **out)
+    assert rlk.check_status(ws) == 0
+    acc = acc.cpu().numpy()
+    for b, r0 in ((0, 0), (1, 3)):
+        assert 0 <= int(tok[r0 + acc[b]]) < 300
+    # fewer drafts than rows: the rest is left as it was
+    a["cu_draft"] = dev([0, 2, 4])
+    out = dict(tokens=dev(np.full(7, 77)), logp=torch.full((7,), 7.0, device="cuda"))
+    tok, acc, logp, ws = rlk.draft_verify(**a, **out)
+    assert rlk.check_status(ws) == 0 and int(tok[6]) == 77 and float(logp[6]) == 7.0
+
+
+def test_verify_reports_bad_rows():
+    def status(**over):
+        a = verify_inputs([2, 2], 5000, "f32", True, 6, 1.0)
+        a["u_accept"].fill_(1 - E)  # nothing that is not likelier than in the draft is accepted
+        for k, f in over.items():
+            f(a[k])
+        tok, acc, logp, ws = rlk.draft_verify(**a)
+        return rlk.check_status(ws), tok.cpu().numpy()
+
+    base, tok0 = status()
+    assert base == 0
+    for val in (math.nan, math.inf):
+        st, tok = status(logits=lambda z: z[0].__setitem__(4999, val))
+        assert st == rlk.DERR_LOGITS and tok[0] == -1
+        np.testing.assert_array_equal(tok[3:], tok0[3:])  # the other sequence is what it was
+    st, tok = status(logits=lambda z: z[3].fill_(-math.inf))
+    assert st == rlk.DERR_LOGITS and tok[3] == -1
+    st, _ = status(draft_logits=lambda z: z[0].__setitem__(0, math.nan))
+    assert st == rlk.DERR_LOGITS
+    for y in (-1, 5000, 2 ** 31 - 1):
+        st, tok = status(draft=lambda d: d.__setitem__(0, y))
+        assert st == rlk.DERR_TARGET and tok[0] == -1
+    st, tok = status(cu_draft=lambda c: c.__setitem__(1, -1))
+    assert st == rlk.DERR_CU_SEQLENS
+    st, tok = status(cu_draft=lambda c: c.__setitem__(2, 9))
+    assert st == rlk.DERR_CU_SEQLENS
+
+
+# ---- streams, graphs ----
+
+def calls(seed, new=3):
+    """One step of the rollout side on its own buffers; returns (run, outputs)."""
+    c, table, lens, cu, gen = build([(90, new), (700, 1), (3, new)], 2, 16, 128, "bf16", seed)
+    T = int(cu[-1])
+    q, k, v = (torch.randn(T, h, 128, generator=gen, device="cuda").to(torch.bfloat16) for h in (8, 2, 2))
+    a = verify_inputs([3, 0, 4], 5001, "bf16", True, seed, 1.0)
+    b = rlk.make_cache(**c, T=T, n_q_heads=8)
+    o = dict(q=torch.empty_like(q), out=torch.empty_like(q), lse=torch.empty(T, 8, device="cuda"), tok=dev(np.zeros(10)),
+             acc=dev(np.zeros(3)), logp=torch.zeros(10, device="cuda"))
+    ws = [rlk.alloc_workspace(rlk.kv_workspace_size(b)) for _ in range(2)]
+    p = rlk.Verify(n_draft=7, B=3, V=5001, dtype=rlk.DTYPE_BF16, temperature=1.0, ld_logits=5001, ld_draft=5001)
+    ws.append(rlk.alloc_workspace(rlk.verify_workspace_size(p)))
+    freq = 1e4 ** (-torch.arange(64, dtype=torch.float64, device="cuda") / 64)
+
+    def run(stream=None):
+        rlk.kv_append(**c, q=q, k=k, v=v, freq=freq, q_out=o["q"], ws=ws[0], stream=stream)
+        rlk.kv_attention(o["q"], **c, out=o["out"], lse=o["lse"], ws=ws[1], stream=stream)
+        rlk.draft_verify(**a, tokens=o["tok"], n_accepted=o["acc"], logp=o["logp"], ws=ws[2], stream=stream)
+
+    return run, o, (q, k, a)
+
+
+@pytest.mark.parametrize("new", [3, 60])
+def test_graph_replay(new):
+    run, o, (q, k, a) = calls(1, new)
+    run()
+    torch.cuda.synchronize()
+    ref = {n: t.clone() for n, t in o.items()}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    x = torch.randn(1024, 1024, device="cuda")
+    for rep in range(4):
+        for t in o.values():
+            t.fill_(7)
+        y = x @ x
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for n, t in o.items():
+            assert torch.equal(t, ref[n]), (rep, n)
+        del y
+    q.mul_(0.5)  # live inputs: the replay follows them
+    k.mul_(0.5)
+    a["u_accept"].fill_(0.0)
+    run()
+    torch.cuda.synchronize()
+    ref2 = {n: t.clone() for n, t in o.items()}
+    assert not torch.equal(ref2["out"], ref["out"])
+    for t in o.values():
+        t.fill_(7)
+    g.replay()
+    torch.cuda.synchronize()
+    for n, t in o.items():
+        assert torch.equal(t, ref2[n]), n
+
+
+def test_two_streams():
+    """Two steps on streams of their own, workspaces of their own, give what they give alone."""
+    a, b = calls(1), calls(2, 40)
+    refs = []
+    for run, o, _ in (a, b):
+        run()
+        torch.cuda.synchronize()
+        refs.append({n: t.clone() for n, t in o.items()})
+        for t in o.values():
+            t.fill_(7)
+    torch.cuda.synchronize()
+    s = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for (run, _, _), st in zip((a, b), s):
+            run(stream=st)
+    torch.cuda.synchronize()
+    for (_, o, _), ref in zip((a, b), refs):
+        for n, t in o.items():
+            assert torch.equal(t, ref[n]), n
+
+
+# ---- run together ----
+
+def test_packed_tree_through_the_cache_gives_each_trajectory_its_log_probs():
+    """One attention layer and the LM head over packed prefix trees, in chunks through the cache, against the same
+    layer over every recorded call's own sequence: the same log-probs of the response tokens; then the loss on them."""
+    from oracle import rl_oracle  # noqa: F401  (the loss itself is held to its oracle elsewhere)
+
+    rng = np.random.default_rng(8)
+    H, K, D, d, V, ps = 4, 2, 32, 128, 96, 16
+    calls_ = []
+    for r in range(3):
+        hist = list(rng.integers(0, V, 40 + 10 * r))
+        turns = []
+        for c in range(5):
+            y = list(rng.integers(0, V, 12 + c))
+            turns.append((list(hist), y))
+            if c == 2:
+                hist = hist[:30]  # the harness dropped the tail: another branch
+            hist = hist + (y if c != 2 else []) + list(rng.integers(0, V, 7))
+        calls_.append(turns)
+    t = rlk.tree_pack(calls_)
+    n = int(t["pos_off"][-1])
+    R = 3
+    emb = torch.as_tensor(rng.standard_normal((V, d)), dtype=torch.float32, device="cuda")
+    wqkv = torch.as_tensor(rng.standard_normal((d, (H + 2 * K) * D)) / math.sqrt(d), dtype=torch.float32, device="cuda")
+    W = torch.as_tensor(rng.standard_normal((V, d)) * 0.3, dtype=torch.float32, device="cuda")
+    wn = torch.as_tensor(1 + 0.1 * rng.standard_normal(D), dtype=torch.float32, device="cuda")
+    freq = 1e4 ** (-torch.arange(0, D, 2, dtype=torch.float64, device="cuda") / D)
+    ends_flat = rlk.tree_ends(t["pos_off"], t["parent"])
+    lens = np.diff(t["pos_off"])
+    used = -(-lens // ps)
+    table = np.zeros((R, used.max()), np.int64)
+    pages = rng.permutation(used.sum())
+    for b in range(R):
+        table[b, :used[b]] = pages[used[:b].sum():used[:b + 1].sum()]
+    ends = np.zeros((R, lens.max()), np.int64)
+    for b in range(R):
+        ends[b, :lens[b]] = ends_flat[t["pos_off"][b]:t["pos_off"][b + 1]]
+    kp, vp = (torch.full((used.sum(), K, ps, D), float("nan"), device="cuda") for _ in range(2))
+    hidden = torch.empty(n, d, device="cuda")
+    done = np.zeros(R, np.int64)
+    while (done < lens).any():  # a chunk of up to 37 positions of every rollout at a time
+        new = np.minimum(37, lens - done)
+        at = np.concatenate([t["pos_off"][b] + done[b] + np.arange(new[b]) for b in range(R)])
+        done += new
+        x = emb[dev(t["token"][at], torch.int64)]
+        qkv = (x @ wqkv).view(-1, H + 2 * K, D)
+        c = dict(k_pages=kp, v_pages=vp, page_table=dev(table), kv_len=dev(done), cu_new=dev(np.concatenate([[0], np.cumsum(new)])))
+        q, ws = rlk.kv_append(**c, q=qkv[:, :H], k=qkv[:, H:H + K], v=qkv[:, H + K:], freq=freq, positions=dev(t["depth"][at]),
+                              q_norm=wn, k_norm=wn)
+        assert rlk.check_status(ws) == 0
+        out, _, ws = rlk.kv_attention(q, **c, slot_end=dev(ends), ws=ws)
+        assert rlk.check_status(ws) == 0
+        hidden[dev(at, torch.int64)] = out.reshape(-1, d) + x
+    rows = hidden[dev(t["row_src"], torch.int64)].contiguous()
+    tgt, mask, cu = dev(t["row_target"]), dev(t["row_mask"], torch.uint8), dev(t["row_cu"])
+    logp, _, _, _ = rlk.logprob_fwd(rows, W, tgt, mask, cu)
+    got = np.zeros(n)
+    src_of = {}
+    lp = logp.cpu().numpy()
+    # the packed position that each row predicts: its position is the row's own, in order, tree roots left out
+    pos = [i for i in range(n) if t["parent"][i] >= 0]
+    for r, i in enumerate(pos):
+        got[i] = lp[r]
+        src_of[i] = r
+
+    def sequence_logp(tokens):
+        x = host(emb)[tokens]
+        y = (x @ host(wqkv)).reshape(len(tokens), H + 2 * K, D)
+        norm = lambda z: z / np.sqrt((z * z).mean(-1, keepdims=True) + 1e-6) * host(wn)  # noqa: E731
+        qq, kk, vv = norm(y[:, :H]), norm(y[:, H:H + K]), y[:, H + K:]
+        for i in range(len(tokens)):
+            qq[i], _ = RO._rotate(qq[i], i * host(freq), "half")
+            kk[i], _ = RO._rotate(kk[i], i * host(freq), "half")
+        o = np.zeros((len(tokens), H, D))
+        for i in range(len(tokens)):
+            for h in range(H):
+                s = kk[:i + 1, h // 2] @ qq[i, h] / math.sqrt(D)
+                e = np.exp(s - s.max())
+                o[i, h] = e @ vv[:i + 1, h // 2] / e.sum()
+        z = (o.reshape(len(tokens), d) + x) @ host(W).T
+        return z - np.log(np.exp(z - z.max(-1, keepdims=True)).sum(-1, keepdims=True)) - z.max(-1, keepdims=True)
+
+    checked = 0
+    for r in range(R):
+        o = int(t["pos_off"][r])
+        for x, y in calls_[r]:
+            tokens = np.array(x + y)
+            # the call's path: its last response token is the packed position whose path spells it
+            for i in range(o, int(t["pos_off"][r + 1])):
+                path, j = [], i
+                while j >= 0:
+                    path.append(j)
+                    j = t["parent"][j]
+                if len(path) == len(tokens) and np.array_equal(t["token"][path[::-1]], tokens):
+                    break
+            else:
+                raise AssertionError("the call is not in the tree")
+            path = path[::-1]
+            full = sequence_logp(tokens)
+            for k in range(len(x), len(tokens)):
+                # fp32 through one layer of 128 wide: products of sums of 128, a few 1e-6 of logits of size ~10
+                assert abs(got[path[k]] - full[k - 1, tokens[k]]) <= 1e-4, (r, k)
+                checked += 1
+    log(f"  {checked} response tokens")
+    rew, gid = torch.tensor([1.0, 0.0, 1.0], device="cuda"), dev([1, 1, 1])
+    loss, dh, dW, ws = rlk.pg_loss_fwd_bwd(rows, W, tgt, mask, cu, logp, rew, gid, rlk.make_params(tis_cap=2.0),
+                                           rollout_logp=logp)
+    assert rlk.check_status(ws) == 0 and bool(torch.isfinite(loss).all()) and float(dW.abs().max()) > 0
+
+
+def test_drafted_step_feeds_the_loss():
+    """Drafts appended as a chunk, attended, verified; the tokens and log-probs go to the loss as they come, and the
+    trainer's own log-probs of those tokens are the verification's."""
+    rng = np.random.default_rng(9)
+    H, K, D, V, B, nd = 4, 2, 32, 1000, 5, 4
+    d = H * D
+    c, table, lens, cu, gen = build([(30 + 11 * b, nd + 1) for b in range(B)], K, 16, D, "f32", 9)
+    T = int(cu[-1])
+    qkv = torch.randn(T, H + 2 * K, D, generator=gen, device="cuda")
+    W = torch.randn(V, d, generator=gen, device="cuda") * 0.4
+    q, ws = rlk.kv_append(**c, q=qkv[:, :H], k=qkv[:, H:H + K], v=qkv[:, H + K:])
+    out, _, ws = rlk.kv_attention(q, **c, max_new=nd + 1, ws=ws)
+    hidden = out.reshape(T, d) * 3
+    z = hidden @ W.T
+    cd = dev(np.arange(B + 1) * nd)
+    at = dev(np.concatenate([b * (nd + 1) + np.arange(nd) for b in range(B)]), torch.int64)
+    zq = z[at] + 0.3 * torch.randn(B * nd, V, generator=gen, device="cuda")
+    draft = (zq + torch.distributions.Gumbel(0.0, 1.0).sample((B * nd, V)).cuda()).argmax(1).to(torch.int32)
+    ua, us = torch.rand(B * nd, generator=gen, device="cuda"), torch.rand(B, generator=gen, device="cuda")
+    tok, acc, logp, _ = rlk.draft_verify(z, draft, cd, ua, us, draft_logits=zq)
+    log(f"  accepted {acc.tolist()}")
+    mask = (tok >= 0).to(torch.uint8)
+    assert mask.view(B, nd + 1).sum(1).tolist() == (acc + 1).tolist()
+    own, _, _, ws = rlk.logprob_fwd(hidden, W, tok.clamp_min(0), mask, dev(cu))
+    assert rlk.check_status(ws) == 0
+    # logits of size 10 from sums of 128 in fp32, made twice
+    assert float((own - logp).abs().max()) <= 1e-4
+    rew, gid = torch.rand(B, generator=gen, device="cuda"), dev([1] * B)
+    loss, _, dW, ws = rlk.pg_loss_fwd_bwd(hidden, W, tok.clamp_min(0), mask, dev(cu), own, rew, gid, rlk.make_params(tis_cap=2.0),
+                                          rollout_logp=logp)
+    assert rlk.check_status(ws) == 0 and bool(torch.isfinite(loss).all()) and float(dW.abs().max()) > 0

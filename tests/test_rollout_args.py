@@ -1,0 +1,182 @@
+"""Refusals of the rollout-side calls: by the binding before the library is reached, and by the C ABI before anything
+is launched (no GPU)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2608_16798_amd as rlk
+
+T, B, H, K, D, PS, NP, MP, V = 6, 2, 4, 2, 16, 4, 5, 3, 40
+bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+
+
+def cache(**over):
+    c = dict(k_pages=torch.zeros(NP, K, PS, D, dtype=bf), v_pages=torch.zeros(NP, K, PS, D, dtype=bf),
+             page_table=torch.zeros(B, MP, dtype=i32), kv_len=torch.tensor([5, 3], dtype=i32),
+             cu_new=torch.tensor([0, 4, 6], dtype=i32))
+    c.update(over)
+    return c
+
+
+def rows(heads, dtype=bf, n=T):
+    return torch.zeros(n, heads, D, dtype=dtype)
+
+
+def append(over=None, **kw):
+    a = dict(q=rows(H), k=rows(K), v=rows(K))
+    a.update(kw)
+    return rlk.kv_append(**cache(**(over or {})), **a)
+
+
+def attend(over=None, **kw):
+    a = dict(q=rows(H))
+    a.update(kw)
+    return rlk.kv_attention(**cache(**(over or {})), **a)
+
+
+def verify(**kw):
+    a = dict(logits=torch.zeros(5, V), draft=torch.zeros(3, dtype=i32), cu_draft=torch.tensor([0, 1, 3], dtype=i32),
+             u_accept=torch.zeros(3), u_sample=torch.zeros(2))
+    a.update(kw)
+    return rlk.draft_verify(**a)
+
+
+BAD = [
+    (append, dict(over=dict(k_pages=torch.zeros(NP, K, PS, D, dtype=torch.float16))), TypeError, "k_pages has dtype"),
+    (append, dict(over=dict(v_pages=torch.zeros(NP, K, PS, D))), TypeError, "v_pages has dtype"),
+    (append, dict(over=dict(v_pages=torch.zeros(NP, K, PS, D + 8, dtype=bf))), ValueError, "v_pages has shape"),
+    (append, dict(over=dict(page_table=torch.zeros(B + 1, MP, dtype=i32))), ValueError, "page_table has shape"),
+    (append, dict(over=dict(page_table=torch.zeros(B, MP, dtype=torch.int64))), TypeError, "page_table has dtype"),
+    (append, dict(over=dict(cu_new=torch.zeros(B, dtype=i32))), ValueError, "cu_new has shape"),
+    (append, dict(over=dict(kv_len=torch.zeros(B))), TypeError, "kv_len has dtype"),
+    (append, dict(over=dict(k_pages=torch.zeros(NP, PS, K, D, dtype=bf).transpose(1, 2))), ValueError, "contiguous"),
+    (append, dict(q=rows(H, f32)), TypeError, "q has dtype"),
+    (append, dict(k=rows(K + 1)), ValueError, "k has shape"),
+    (append, dict(v=rows(K, n=T + 1)), ValueError, "v has shape"),
+    (append, dict(q=torch.zeros(H, T, D, dtype=bf).transpose(0, 1)), ValueError, "heads of a token together"),
+    (append, dict(q=torch.zeros(T, H, 2 * D, dtype=bf)[:, :, ::2]), ValueError, "heads of a token together"),
+    (append, dict(q=None, q_out=rows(H)), ValueError, "q_out without q"),
+    (append, dict(q_out=rows(H, f32)), TypeError, "q_out has dtype"),
+    (append, dict(freq=torch.zeros(8)), TypeError, "freq has dtype"),
+    (append, dict(positions=torch.zeros(T, dtype=torch.int64)), TypeError, "positions has dtype"),
+    (append, dict(positions=torch.zeros(T - 1, dtype=i32)), ValueError, "positions has shape"),
+    (append, dict(q_norm=torch.zeros(D)), TypeError, "q_norm has dtype"),
+    (append, dict(k_norm=torch.zeros(D - 8, dtype=bf)), ValueError, "k_norm has shape"),
+    (append, dict(rot_style="neither"), ValueError, "rot_style"),
+    (append, dict(), ValueError, "must be a GPU tensor"),
+    (attend, dict(q=rows(H, f32)), TypeError, "q has dtype"),
+    (attend, dict(q=torch.zeros(T, H, D + 8, dtype=bf)), ValueError, "q has shape"),
+    (attend, dict(slot_end=torch.zeros(B, 8)), TypeError, "slot_end has dtype"),
+    (attend, dict(slot_end=torch.zeros(B + 1, 8, dtype=i32)), ValueError, "slot_end has shape"),
+    (attend, dict(out=rows(H + 1)), ValueError, "out has shape"),
+    (attend, dict(lse=torch.zeros(T, H + 1)), ValueError, "lse has shape"),
+    (attend, dict(ws=torch.zeros(64)), TypeError, "ws has dtype"),
+    (attend, dict(), ValueError, "must be a GPU tensor"),
+    (verify, dict(logits=torch.zeros(4, V)), ValueError, "expected n_draft . B = 5"),
+    (verify, dict(logits=torch.zeros(5, V, dtype=torch.float64)), TypeError, "logits has dtype"),
+    (verify, dict(logits=torch.zeros(V, 5).t()), ValueError, "contiguous"),
+    (verify, dict(draft=torch.zeros(3, dtype=torch.int64)), TypeError, "draft has dtype"),
+    (verify, dict(u_accept=torch.zeros(2)), ValueError, "u_accept has shape"),
+    (verify, dict(u_sample=torch.zeros(2, dtype=torch.float64)), TypeError, "u_sample has dtype"),
+    (verify, dict(cu_draft=torch.zeros(2, dtype=i32)), ValueError, "cu_draft has shape"),
+    (verify, dict(draft_logits=torch.zeros(3, V, dtype=bf)), TypeError, "draft_logits has dtype"),
+    (verify, dict(draft_logits=torch.zeros(3, V + 1)), ValueError, "draft_logits has shape"),
+    (verify, dict(tokens=torch.zeros(4, dtype=i32)), ValueError, "tokens has shape"),
+    (verify, dict(), ValueError, "must be a GPU tensor"),
+]
+
+
+@pytest.mark.parametrize("call,kw,exc,msg", BAD, ids=[f"{b[0].__name__}-{b[3]}-{i}" for i, b in enumerate(BAD)])
+def test_binding_rejects(monkeypatch, call, kw, exc, msg):
+    def refuse(*a, **k):
+        raise AssertionError("the C ABI was reached")
+
+    monkeypatch.setattr(rlk, "load_library", refuse)
+    with pytest.raises(exc, match=msg):
+        call(**kw)
+
+
+FAKE = 0x10000  # never dereferenced: every call below fails validation first
+
+
+def c_cache(**over):
+    f = dict(T=T, B=B, n_pages=NP, page_size=PS, max_pages=MP, n_q_heads=H, n_kv_heads=K, head_dim=D, dtype=rlk.DTYPE_BF16,
+             k_pages=FAKE, v_pages=FAKE, page_table=FAKE, kv_len=FAKE, cu_new=FAKE)
+    f.update(over)
+    return rlk.KvCache(**f)
+
+
+def c_append(c, r=None, q=FAKE, qs=H * D, k=FAKE, ks=K * D, v=FAKE, vs=K * D, q_out=FAKE + 4096, ws=FAKE, n=1 << 30, rot=True):
+    r = r or rlk.Rotation(freq=FAKE, rot_dim=D, norm_eps=1e-6)
+    return rlk.load_library().rlk_kv_append(ctypes.byref(c) if c else None, ctypes.byref(r) if rot else None, q, qs, k, ks, v,
+                                            vs, None, q_out, ws, n, None)
+
+
+def c_attend(c, q=FAKE, qs=H * D, end=None, es=0, scale=0.25, out=FAKE + 4096, ws=FAKE, n=1 << 40):
+    return rlk.load_library().rlk_kv_attention(ctypes.byref(c) if c else None, q, qs, end, es, scale, out, None, ws, n, None)
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("dtype", 7, rlk.RLK_EDTYPE), ("T", -1, rlk.RLK_ESHAPE), ("T", 1 << 31, rlk.RLK_ESHAPE), ("B", -1, rlk.RLK_ESHAPE),
+    ("B", 16385, rlk.RLK_ESHAPE), ("page_size", 0, rlk.RLK_ESHAPE), ("page_size", 12, rlk.RLK_ESHAPE),
+    ("page_size", 2048, rlk.RLK_ESHAPE), ("n_pages", -1, rlk.RLK_ESHAPE), ("max_pages", -1, rlk.RLK_ESHAPE),
+    ("max_pages", 1 << 29, rlk.RLK_ESHAPE), ("head_dim", 0, rlk.RLK_ESHAPE), ("head_dim", 20, rlk.RLK_ESHAPE),
+    ("head_dim", 264, rlk.RLK_ESHAPE), ("n_kv_heads", 0, rlk.RLK_ESHAPE), ("n_q_heads", 3, rlk.RLK_ESHAPE),
+    ("n_q_heads", 0, rlk.RLK_ESHAPE), ("n_q_heads", 2 * 129, rlk.RLK_ESHAPE), ("max_new", -1, rlk.RLK_EINVAL),
+    ("reserved", 1, rlk.RLK_EINVAL), ("kv_len", None, rlk.RLK_EINVAL), ("cu_new", None, rlk.RLK_EINVAL),
+    ("page_table", None, rlk.RLK_EINVAL), ("k_pages", None, rlk.RLK_EINVAL), ("v_pages", FAKE + 8, rlk.RLK_EINVAL)])
+def test_cache_descriptor_rejected(field, value, code):
+    c = c_cache(**{field: value})
+    assert c_append(c) == code
+    assert c_attend(c) == code
+
+
+def test_append_and_attention_reject():
+    assert ctypes.sizeof(rlk.KvCache) == 88 and ctypes.sizeof(rlk.Rotation) == 40 and ctypes.sizeof(rlk.Verify) == 40
+    c = c_cache()
+    lib = rlk.load_library()
+    n = ctypes.c_size_t()
+    assert lib.rlk_kv_workspace_size(ctypes.byref(c), None) == rlk.RLK_EINVAL
+    assert lib.rlk_kv_workspace_size(None, ctypes.byref(n)) == rlk.RLK_EINVAL
+    need = rlk.kv_workspace_size(c)
+    assert need >= 256
+    R = rlk.Rotation
+    EI, ES, EW = rlk.RLK_EINVAL, rlk.RLK_ESHAPE, rlk.RLK_EWORKSPACE
+    for kw, code in ((dict(rot=False), EI), (dict(r=R(freq=FAKE, rot_dim=8)), ES), (dict(r=R(freq=FAKE, rot_dim=32)), ES),
+                     (dict(r=R(freq=FAKE, rot_dim=-16)), ES), (dict(r=R(freq=FAKE, rot_dim=4, rot_style=1)), ES),
+                     (dict(r=R(freq=FAKE, rot_dim=16, rot_style=2)), EI), (dict(r=R(rot_dim=16)), EI),
+                     (dict(r=R(norm_eps=-1.0)), EI), (dict(r=R(norm_eps=float("nan"))), EI), (dict(r=R(q_norm=FAKE + 2)), EI),
+                     (dict(r=R(reserved=1)), EI), (dict(k=None), EI), (dict(v=None), EI), (dict(q=None), EI),
+                     (dict(q_out=None), EI), (dict(k=FAKE + 8), EI), (dict(ks=K * D - 8), ES), (dict(vs=K * D + 4), ES),
+                     (dict(qs=0), ES), (dict(q_out=FAKE, qs=H * D + 8), EI), (dict(q_out=FAKE + 8), EI), (dict(ws=None), EW),
+                     (dict(ws=FAKE + 8), EW), (dict(n=16), EW)):
+        assert c_append(c, **kw) == code, kw
+    for kw, code in ((dict(q=None), EI), (dict(out=None), EI), (dict(out=FAKE), EI), (dict(out=FAKE + 8), EI),
+                     (dict(scale=float("inf")), EI), (dict(scale=float("nan")), EI), (dict(end=FAKE, es=-1), ES),
+                     (dict(qs=H * D + 4), ES), (dict(ws=None), EW), (dict(ws=FAKE + 8), EW), (dict(n=need - 1), EW)):
+        assert c_attend(c, **kw) == code, kw
+    assert c_append(None) == EI and c_attend(None) == EI
+
+
+def test_verify_rejects():
+    lib = rlk.load_library()
+
+    def call(logits=FAKE, dl=None, draft=FAKE, cu=FAKE, ua=FAKE, us=FAKE, tok=FAKE, na=FAKE, lp=FAKE, ws=FAKE, n=1 << 40, **kw):
+        f = dict(n_draft=3, B=2, V=V, dtype=rlk.DTYPE_F32, temperature=1.0, ld_logits=V, ld_draft=V)
+        f.update(kw)
+        p = rlk.Verify(**f)
+        return lib.rlk_draft_verify(ctypes.byref(p), logits, dl, draft, cu, ua, us, tok, na, lp, ws, n, None)
+
+    EI, ES, EW = rlk.RLK_EINVAL, rlk.RLK_ESHAPE, rlk.RLK_EWORKSPACE
+    for kw, code in ((dict(dtype=3), rlk.RLK_EDTYPE), (dict(V=0), ES), (dict(V=(1 << 21) + 1), ES), (dict(B=-1), ES),
+                     (dict(B=16385), ES), (dict(n_draft=-1), ES), (dict(B=0), ES), (dict(n_draft=1 << 30), ES),
+                     (dict(temperature=-1.0), EI), (dict(temperature=float("inf")), EI), (dict(temperature=float("nan")), EI),
+                     (dict(ld_logits=V - 1), ES), (dict(dl=FAKE, ld_draft=V - 1), ES), (dict(logits=None), EI),
+                     (dict(draft=None), EI), (dict(cu=None), EI), (dict(ua=None), EI), (dict(us=None), EI), (dict(tok=None), EI),
+                     (dict(na=None), EI), (dict(lp=None), EI), (dict(logits=FAKE + 8), EI), (dict(dl=FAKE + 4), EI),
+                     (dict(ws=None), EW), (dict(ws=FAKE + 16), EW), (dict(n=64), EW)):
+        assert call(**kw) == code, kw
+    n = ctypes.c_size_t()
+    assert lib.rlk_verify_workspace_size(None, ctypes.byref(n)) == EI
+    assert lib.rlk_draft_verify(None, *([None] * 10), 0, None) == EI
