@@ -1,9 +1,9 @@
-// Rollout side: the append of a chunk of new tokens to the paged key/value cache (per-head norm and position
-// rotation on the way) and the chunk's attention over the cache.
+// Rollout side: the append of a chunk of new tokens to the paged key/value cache, with per-head norm and position
+// rotation on the way.
 //
 // Pools are [n_pages, n_kv_heads, page_size, head_dim]: the keys of one head in a page lie together, so an
-// attention workgroup streams whole lines.  A workgroup never trusts device data: sequences whose offsets or
-// lengths do not fit are skipped, page indices outside the pool are not followed, and both set status bits.
+// attention workgroup streams whole lines.  Device data is not trusted: sequences whose offsets or lengths do not
+// fit are skipped, page indices outside the pool are not followed, and both set status bits.
 #include "rlk_internal.h"
 
 #include <math.h>
@@ -11,8 +11,6 @@
 namespace rlk {
 
 namespace {
-
-__device__ __forceinline__ float bf16_to_f(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   bf16x2 v;
@@ -49,12 +47,6 @@ __device__ __forceinline__ u32x4 pack(const float* f) {
   return v;
 }
 
-template <typename T>
-__device__ __forceinline__ float load1(const T* p) {
-  if constexpr (sizeof(T) == 2) return bf16_to_f(p->bits);
-  else return *p;
-}
-
 // Rows, count and length of sequence b: n = 0 where the sequence is empty or its numbers do not fit.
 struct Seq {
   int row0, n, len;
@@ -67,9 +59,8 @@ __device__ __forceinline__ Seq sequence(const KvArgs& a, int b, int* bad = nullp
   return {r0, rows && fits ? r1 - r0 : 0, len};
 }
 
-// Status bits of the whole call, by one workgroup: offsets, lengths and the pages of the slots from `first` new
-// token (append) or from slot 0 (attention) on.
-__device__ void check_cache(const KvArgs& a, bool new_only, int32_t* status) {
+// Status bits of the whole call, by one workgroup: offsets, lengths and the pages that take new tokens.
+__device__ void check_cache(const KvArgs& a, int32_t* status) {
   __shared__ int s_bad;
   if (threadIdx.x == 0) s_bad = 0;
   __syncthreads();
@@ -79,7 +70,7 @@ __device__ void check_cache(const KvArgs& a, bool new_only, int32_t* status) {
   for (int b = threadIdx.x >> 6; b < a.B; b += nw) {
     const Seq s = sequence(a, b, &bad);
     if (s.n == 0) continue;
-    const int p0 = new_only ? (s.len - s.n) >> a.ps_shift : 0, p1 = (s.len - 1) >> a.ps_shift;
+    const int p0 = (s.len - s.n) >> a.ps_shift, p1 = (s.len - 1) >> a.ps_shift;
     for (int p = p0 + lane; p <= p1; p += 64)
       if ((uint32_t)a.table[(int64_t)b * a.max_pages + p] >= (uint32_t)a.n_pages) bad |= RLK_DERR_PAGE;
   }
@@ -101,7 +92,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) k_kv_append(KvArgs a, RotArgs r, int lg, int tpb, int32_t* status) {
   constexpr int EPC = kEpc<T>;
   if (blockIdx.x == gridDim.x - 1) {
-    check_cache(a, true, status);
+    check_cache(a, status);
     return;
   }
   __shared__ float2 s_cs[kAppendTokens][128];
@@ -238,73 +229,6 @@ __global__ void __launch_bounds__(256) k_kv_append(KvArgs a, RotArgs r, int lg, 
   }
 }
 
-// ---------------------------------------------------------------- attention
-
-__global__ void __launch_bounds__(1024) k_kv_check(KvArgs a, int32_t* status) { check_cache(a, false, status); }
-
-// One wavefront per token and query head, 64 keys at a time: a lane scores a key, then adds up its share of the
-// head's elements.
-template <typename T>
-__global__ void __launch_bounds__(64) k_kv_attention(KvArgs a, AttnArgs p) {
-  __shared__ float s_q[256];
-  __shared__ float s_p[64];
-  __shared__ int s_b;
-  const int64_t t = blockIdx.x;
-  const int h = blockIdx.y, lane = threadIdx.x;
-  int cnt = 0;
-  for (int b = lane; b < a.B; b += 64) cnt += a.cu[b + 1] <= t;
-  for (int o = 32; o > 0; o >>= 1) cnt += __shfl_xor(cnt, o, 64);
-  if (cnt >= a.B) return;
-  const Seq s = sequence(a, cnt);
-  const int64_t i = t - s.row0;
-  if (i < 0 || i >= s.n) return;
-  const int slot = s.len - s.n + (int)i, kh = h / (a.Hq / a.Hkv);
-  for (int e = lane; e < a.D; e += 64) s_q[e] = load1((const T*)p.q + t * p.q_stride + (int64_t)h * a.D + e);
-  __syncthreads();
-  float m = -INFINITY, l = 0.0f, acc[4] = {};
-  const int64_t head_step = (int64_t)a.D << a.ps_shift;
-  for (int j0 = 0; j0 <= slot; j0 += 64) {
-    const int j = j0 + lane;
-    bool see = j <= slot;
-    int64_t at = 0;
-    if (see) {
-      const int page = a.table[(int64_t)cnt * a.max_pages + (j >> a.ps_shift)];
-      if ((uint32_t)page >= (uint32_t)a.n_pages) see = false;
-      else at = (int64_t)page * a.Hkv * head_step + kh * head_step + (int64_t)(j & ((1 << a.ps_shift) - 1)) * a.D;
-      if (p.slot_end && slot >= p.slot_end[cnt * p.end_stride + j]) see = false;
-    }
-    float x = -INFINITY;
-    if (see) {
-      float d = 0.0f;
-      for (int e = 0; e < a.D; ++e) d += s_q[e] * load1((const T*)a.k_pages + at + e);
-      x = d * p.scale;
-    }
-    float mx = x;
-    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-    const float m2 = fmaxf(m, mx), base = m2 == -INFINITY ? 0.0f : m2;
-    const float pj = see ? expf(x - base) : 0.0f, al = expf(m - base);
-    float sum = pj;
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    l = l * al + sum;
-    m = m2;
-    for (int k = 0; k < 4; ++k) acc[k] *= al;
-    for (int jj = 0; jj < 64; ++jj) {
-      const float pv = __shfl(pj, jj, 64);
-      const int64_t av = __shfl(at, jj, 64);
-      if (!__shfl((int)see, jj, 64)) continue;
-      for (int k = 0; k * 64 + lane < a.D; ++k) acc[k] += pv * load1((const T*)a.v_pages + av + k * 64 + lane);
-    }
-  }
-  const bool none = l == 0.0f;
-  for (int k = 0; k * 64 + lane < a.D; ++k) {
-    const float o = none ? 0.0f : acc[k] / l;
-    T* dst = (T*)p.out + (t * a.Hq + h) * a.D + k * 64 + lane;
-    if constexpr (sizeof(T) == 2) dst->bits = __builtin_bit_cast(uint16_t, (__bf16)o);
-    else *dst = o;
-  }
-  if (lane == 0 && p.lse) p.lse[t * a.Hq + h] = none ? -INFINITY : m + logf(l);
-}
-
 }  // namespace
 
 hipError_t launch_kv_append(int dtype, const KvArgs& a, const RotArgs& r, int32_t* status, hipStream_t s) {
@@ -317,18 +241,6 @@ hipError_t launch_kv_append(int dtype, const KvArgs& a, const RotArgs& r, int32_
   if (dtype == RLK_DTYPE_BF16) k_kv_append<bf16_t><<<grid, 256, 0, s>>>(a, r, lg, tpb, status);
   else k_kv_append<float><<<grid, 256, 0, s>>>(a, r, lg, tpb, status);
   prof_mark(KK_KV_APPEND, false, s);
-  return hipGetLastError();
-}
-
-hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, int32_t* status, hipStream_t s) {
-  prof_mark(KK_KV_ATTENTION, true, s);
-  k_kv_check<<<1, 1024, 0, s>>>(a, status);
-  const dim3 grid((unsigned)a.T, (unsigned)a.Hq);
-  if (a.T > 0) {
-    if (dtype == RLK_DTYPE_BF16) k_kv_attention<bf16_t><<<grid, 64, 0, s>>>(a, p);
-    else k_kv_attention<float><<<grid, 64, 0, s>>>(a, p);
-  }
-  prof_mark(KK_KV_ATTENTION, false, s);
   return hipGetLastError();
 }
 

@@ -1,0 +1,882 @@
+// Rollout side: attention of a chunk's new tokens over the paged cache.
+//
+// One pass over the keys with the running maximum m and sum l of the softmax.  Scores are formed transposed, S^T = K Q^T
+// (32 keys x 32 query rows, MFMA 32x32), so a lane owns one query row: its maximum and sum are in-lane up to one
+// exchange between the wavefront's halves, its rescaling factor is one register, and the probabilities already lie as
+// the second product O^T = V^T P^T takes them (B operand; the order of the keys inside a product is free, so V's rows
+// are read in the order that S^T left them).  P never leaves the registers.
+//
+// Query heads that share a key head are rows of one tile: row r of a tile is token r / g, head r % g of the group of g.
+// Keys and values go from their pages to LDS by DMA, tiles ahead, and are read from there as fragments (values by
+// transposing reads).
+//
+// Work is cut by cost, not by sequence: the row tiles of all sequences and key heads, each with the keys it sees, lie in
+// one line that every workgroup takes an equal piece of.  A tile cut between workgroups leaves partial sums that
+// k_kv_merge joins in order.  One token over a long history and a batch of ragged ones are the same to it.
+#include "rlk_internal.h"
+
+#include <math.h>
+
+#include <algorithm>
+#include <mutex>
+#include <type_traits>
+
+namespace rlk {
+
+namespace {
+
+constexpr float kLn2f = 0.6931471805599453f, kLog2ef = 1.4426950408889634f;
+constexpr int kPageCap = 1024;     // page indices held in LDS
+constexpr int kItemCost = 96;      // cost of starting a row tile, in keys
+constexpr float kLazy = 8.0f;      // the maximum may be passed by 2^8 before the sums are rescaled
+
+#define LDSP(p) ((__attribute__((address_space(3))) void*)(p))
+
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+  bf16x2 v;
+  v.x = (__bf16)lo;
+  v.y = (__bf16)hi;
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// Waits until at most M vector-memory operations are in flight (63: the most that the counter's field says).
+template <int M>
+__device__ __forceinline__ void wait_vmcnt() {
+  constexpr int N = M < 63 ? M : 63;
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+}
+
+// Workgroup barrier that leaves copies in flight.
+__device__ __forceinline__ void block_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Maximum / sum of a lane and the one 32 further.
+__device__ __forceinline__ float swap_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float swap_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Rows, new tokens and cached tokens before them; n = 0 where the numbers do not fit (see k_kv.hip).
+struct Seq {
+  int row0, n, len;
+};
+__device__ __forceinline__ Seq sequence(const KvArgs& a, int b, int* bad = nullptr) {
+  const int r0 = a.cu[b], r1 = a.cu[b + 1], len = a.kv_len[b];
+  const bool rows = r0 >= 0 && r1 >= r0 && r1 <= a.T;
+  const bool fits = len >= 0 && len <= a.cap && (!rows || len >= r1 - r0);
+  if (bad) *bad |= (rows ? 0 : RLK_DERR_CU_SEQLENS) | (fits ? 0 : RLK_DERR_KV_LEN);
+  return {r0, rows && fits ? r1 - r0 : 0, len};
+}
+
+// Geometry of a tile: DP = head_dim rounded up to 64, 128 or 256; a row of it in LDS has CPR 16-byte chunks.
+template <typename T, int DP>
+struct Geo {
+  static constexpr int ESZ = sizeof(T), EPC = 16 / ESZ, CPR = DP / EPC, ROWB = DP * ESZ, RPI = 1024 / ROWB;
+  // Chunk swizzles.  K: a fragment read takes the same chunk of 16 consecutive rows at a time; they have to lie in
+  // different 16-byte banks of the 256-byte window.  V (bf16): a transposing read takes 32 bytes of each of four rows
+  // for 16 lanes, the neighbouring 32 bytes for the next 16.  V (fp32): rows 4 apart are read together, 128 bytes each.
+  static __device__ __forceinline__ int k_swz(int row) { return CPR == 8 ? (row >> 1) & 7 : row & 15; }
+  static __device__ __forceinline__ int v_swz(int row) {
+    if (ESZ == 4) return (row & 4) << 1;
+    return CPR == 8 ? (row & 2) << 1 : (row & 3) << 2;
+  }
+};
+
+// WM x WK wavefronts: WM groups of 32 query rows, WK groups of 32 NB keys; NS stages of tiles in LDS.
+template <typename T, int DP_, int WM_, int WK_, int NB_, int NS_>
+struct Cfg : Geo<T, DP_> {
+  typedef Geo<T, DP_> G;
+  static constexpr int DP = DP_, WM = WM_, WK = WK_, NB = NB_, NS = NS_;
+  static constexpr int WAVES = WM * WK, BM = 32 * WM, PK = 32 * NB, TK = PK * WK;  // rows, keys of a part, of a tile
+  static constexpr int LROWS = PK / WM, NI = LROWS / G::RPI;                       // a wavefront's share of the copies
+  static constexpr int PART = PK * G::ROWB, STAGE = 2 * PART * WK;                 // bytes of K (or V) of a part; of a stage
+  static constexpr int ENDS = NS * STAGE;                                          // int [NS][TK]: slot_end of the keys
+  static constexpr int PAGES = ENDS + NS * TK * 4;                                 // int [kPageCap]
+  static constexpr int FLAG = PAGES + kPageCap * 4;                                // int [NS][8]: non-finite values
+  static constexpr int MISC = FLAG + NS * 8 * 4;
+  static constexpr int LDS = MISC + 64;
+  // joining the key groups: fp32 [WK][32][DP + 4] and m, l [WK][32], in the stages
+  static constexpr int OROW = DP + 4;
+  static_assert(WK == 1 || WK * 32 * OROW * 4 + WK * 32 * 8 <= NS * STAGE, "joining fits the stages");
+  static_assert(WM == 1 || WK == 1, "rows or keys are split");
+  static_assert(NI >= 1 && NI * G::RPI * WM == PK, "copies");
+};
+
+// ds_read_b64_tr_b16: 16 lanes address four rows (lane / 4), 8 bytes each (lane % 4); lane i gets column i of the four.
+// Values of 16 keys (two groups of four per half) for the four or two 32-wide blocks of the head that share the bank
+// pattern: eight (four) reads and their wait in one statement, since the compiler would wait for every copy in flight
+// before a transposing read of its own (it takes the read to alias the copies' LDS writes).
+template <int N, int OFF, int STEP>
+__device__ __forceinline__ void read_v(const int (&u)[N], u32x4 (&f)[N]) {
+  u32x2 l[N], h[N];
+  if constexpr (N == 4) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %4, %8 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %1, %9 offset:%12\n\tds_read_b64_tr_b16 %5, %9 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %2, %10 offset:%12\n\tds_read_b64_tr_b16 %6, %10 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %3, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(l[3]), "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3])
+        : "v"(u[0]), "v"(u[1]), "v"(u[2]), "v"(u[3]), "i"(OFF), "i"(OFF + STEP)
+        : "memory");
+  } else {
+    static_assert(N == 2, "blocks of a read");
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %2, %4 offset:%7\n\t"
+        "ds_read_b64_tr_b16 %1, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(h[0]), "=&v"(h[1])
+        : "v"(u[0]), "v"(u[1]), "i"(OFF), "i"(OFF + STEP)
+        : "memory");
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = u32x4{l[i].x, l[i].y, h[i].x, h[i].y};
+}
+
+// Infinities and NaN of a fragment of values are taken out of it: a zero probability times one of them is NaN, so a row
+// that does not see the key would get it too.  They come back as counts (up: +inf, down: -inf, NaN in both) against
+// the probabilities' signs.
+__device__ __forceinline__ void take_nonfinite(u32x4& v, u32x4& up, u32x4& down) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t x = v[w];
+    const uint32_t odd = ((((x & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xffffu;   // exponent all ones
+    const uint32_t nan = ((((x & 0x007f007fu) + 0x007f007fu) >> 7) & 0x00010001u) * 0xffffu;    // and a mantissa
+    const uint32_t neg = ((x >> 15) & 0x00010001u) * 0xffffu;
+    up[w] = odd & (nan | ~neg) & 0x3f803f80u;
+    down[w] = odd & (nan | neg) & 0x3f803f80u;
+    v[w] = x & ~odd;
+  }
+}
+
+// Key of register r of a 32 x 32 result in the lanes of half h.
+__device__ __forceinline__ constexpr int key_of(int r, int h) { return (r & 3) + 8 * (r >> 2) + 4 * h; }
+
+// The line of work.  A row tile with v visible keys costs v + kItemCost; a sequence of n new tokens after ctx cached ones
+// has tiles of tpt tokens whose v grows by tpt (the last one's is rounded up: only the cut uses it).
+__device__ __forceinline__ int64_t tiles_cost(int64_t t, int64_t ctx, int64_t tpt) {
+  return t * (ctx + kItemCost) + tpt * (t * (t + 1) / 2);
+}
+
+template <typename C>
+__device__ __forceinline__ int64_t block_exclusive(int64_t v, char* smem, int64_t* total) {
+  int64_t* s = reinterpret_cast<int64_t*>(smem);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int64_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 63) s[w] = incl;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+  for (int k = 0; k < C::WAVES; ++k) {
+    if (k < w) before += s[k];
+    all += s[k];
+  }
+  __syncthreads();
+  *total = all;
+  return before + incl - v;
+}
+
+// A row tile that its first workgroup did not end.
+struct MergeDesc {
+  int32_t b, h, rt, last;  // last workgroup with a part of the tile; -1: nothing to join
+};
+
+struct AttnPlan {
+  int tpt;            // tokens of a row tile
+  int64_t min_piece;  // least cost of a workgroup
+  MergeDesc* desc;    // [workgroups]
+  int32_t* flags;     // [workgroups]: status bits
+  float2* ml;         // [2 workgroups][BM]: maximum (powers of 2) and sum of a part: 2 w the tail of a tile, 2 w + 1 its head
+  float* part;        // [2 workgroups][BM][DP]
+  int32_t* status;
+};
+
+template <typename C>
+constexpr int DP_OF = C::DP;
+
+template <typename T, typename C>
+__global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 256 ? 2 : 1)) k_kv_attn(KvArgs a, AttnArgs p, AttnPlan pl) {
+  typedef typename C::G G;
+  constexpr int ESZ = G::ESZ, EPC = G::EPC, CPR = G::CPR, DP = C::DP, NB = C::NB, NI = C::NI, NS = C::NS, DB = DP / 32;
+  extern __shared__ __align__(1024) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = C::WM > 1 ? wid : 0, kw = C::WK > 1 ? wid : 0;
+  const int hl = lane >> 5, ql = lane & 31;
+  int* s_pages = reinterpret_cast<int*>(smem + C::PAGES);
+  int* s_ends = reinterpret_cast<int*>(smem + C::ENDS);
+  int* s_flag = reinterpret_cast<int*>(smem + C::FLAG);
+  const int g = a.Hq / a.Hkv, tpt = pl.tpt;
+
+  const int nwg = gridDim.x;  // a multiple of 8
+  int wg;
+  // ---- this workgroup's piece of the line
+  int64_t tot, piece, lo, hi;
+  __shared__ int s_b;
+  __shared__ int64_t s_before;
+  {
+    const int per = (a.B + C::WAVES * 64 - 1) / (C::WAVES * 64);
+    const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) {
+      const Seq s = sequence(a, b);
+      mine += tiles_cost((s.n + tpt - 1) / tpt, s.len - s.n, tpt);
+    }
+    const int64_t before = block_exclusive<C>(mine, smem, &tot);
+    const int64_t all = tot * a.Hkv;
+    piece = (all + nwg - 1) / nwg;
+    if (piece < pl.min_piece) piece = pl.min_piece;
+    // The workgroups of one XCD (ids equal mod 8) take neighbouring pieces, which share keys in its L2; the pieces in
+    // use are spread evenly over the XCDs, and who has none comes behind them.
+    const int xcd = blockIdx.x & 7, nth = blockIdx.x >> 3;
+    const int used = (int)((all + piece - 1) / piece), each = (used + 7) / 8;
+    wg = nth < each ? xcd * each + nth : nth * 8 + xcd;
+    lo = piece * wg;
+    hi = min(all, lo + piece);
+    if (lo < hi) {
+      const int64_t x = lo % tot;
+      if (x >= before && x < before + mine) {
+        int64_t at = before;
+        for (int b = b0; b < b1; ++b) {
+          const Seq s = sequence(a, b);
+          const int64_t c = tiles_cost((s.n + tpt - 1) / tpt, s.len - s.n, tpt);
+          if (x < at + c) {
+            s_b = b;
+            s_before = at;
+            break;
+          }
+          at += c;
+        }
+      }
+    }
+    __syncthreads();
+  }
+  MergeDesc* desc = pl.desc + wg;
+  if (lo >= hi) {
+    if (tid == 0) {
+      *desc = {0, 0, 0, -1};
+      pl.flags[wg] = 0;
+    }
+    return;
+  }
+  int b = __builtin_amdgcn_readfirstlane(s_b), h = (int)(lo / tot);
+  Seq s = sequence(a, b);
+  int64_t start = h * tot + s_before;  // cost before the sequence; below: before the tile
+  int rt = 0;
+  {
+    // the tile that holds lo: the last t with tiles_cost(t) <= lo - start
+    const int64_t x = lo - start, ctx = s.len - s.n;
+    int t0 = 0, t1 = (s.n + tpt - 1) / tpt;  // cost(t0) <= x < cost(t1)
+    while (t1 - t0 > 1) {
+      const int m = (t0 + t1) >> 1;
+      if (tiles_cost(m, ctx, tpt) <= x) t0 = m;
+      else t1 = m;
+    }
+    rt = t0;
+    start += tiles_cost(t0, ctx, tpt);
+  }
+
+  // ---- lane constants
+  const int64_t row_bytes = (int64_t)a.D * ESZ;
+  const int64_t head_bytes = row_bytes << a.ps_shift, page_bytes = a.Hkv * head_bytes;
+  const bool paged_rows = (1 << a.ps_shift) >= G::RPI;  // the rows of a copy lie in one page
+  const int crow = lane / CPR, cchunk = lane % CPR;
+  // key and value fragments
+  const int k_base = kw * C::PART + ql * G::ROWB + ((hl ^ G::k_swz(ql)) << 4);
+  int v_base[DB < 4 ? DB : 4];
+  constexpr int VB = DB < 4 ? DB : 4;
+  {
+    const int i = lane & 15, r = i >> 2;
+#pragma unroll
+    for (int d = 0; d < VB; ++d) {
+      const int pair = (d * 2 + ((lane >> 4) & 1)) ^ (G::v_swz(r) >> 1);
+      v_base[d] = (int)(uintptr_t)LDSP(smem) + (C::WK + kw) * C::PART + (4 * hl + r) * G::ROWB + pair * 32 + (i & 3) * 8;
+    }
+  }
+  const float c = fabsf(p.scale) > 0.0f ? fabsf(p.scale) * kLog2ef : 1.0f;
+  const float sign = p.scale > 0.0f ? 1.0f : p.scale < 0.0f ? -1.0f : 0.0f;
+  int bad = 0;
+  MergeDesc md = {0, 0, 0, -1};
+
+  for (;;) {
+    // ---- item: row tile rt of sequence b, key head h
+    const int ctx = s.len - s.n;
+    const int tok0 = rt * tpt, ntok = min(tpt, s.n - tok0);
+    const int vis = ctx + tok0 + ntok;
+    const int64_t cost = (int64_t)ctx + (int64_t)(rt + 1) * tpt + kItemCost;
+    const int kt = (vis + C::TK - 1) / C::TK;
+    const int64_t x0 = lo > start ? lo - start : 0, x1 = min(hi - start, cost);
+    const int k0 = (int)(x0 * kt / cost), k1 = x1 == cost ? kt : (int)(x1 * kt / cost);
+    const bool whole = x0 == 0 && x1 == cost;
+
+    // query rows of this wavefront: token tok0 + row / g, head h g + row % g
+    const int row = wm * 32 + ql, rtok = row / g;
+    const bool live = rtok < ntok;
+    const int qslot = ctx + tok0 + min(rtok, ntok - 1);
+    const int first_slot = ctx + tok0 + min((wm * 32) / g, ntok - 1);       // of the wavefront's rows
+    const int last_slot = ctx + tok0 + min((wm * 32 + 31) / g, ntok - 1);
+    u32x4 qf[CPR / 2];
+    {
+      const T* q = (const T*)p.q + (int64_t)(s.row0 + tok0 + rtok) * p.q_stride + (int64_t)(h * g + row % g) * a.D;
+#pragma unroll
+      for (int ks = 0; ks < CPR / 2; ++ks) {
+        const int e = (2 * ks + hl) * EPC;
+        qf[ks] = live && e < a.D ? *reinterpret_cast<const u32x4*>(q + e) : u32x4{0, 0, 0, 0};
+        if (sign != 1.0f) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            if constexpr (ESZ == 4) qf[ks][w] = __float_as_uint(__uint_as_float(qf[ks][w]) * sign);
+            else qf[ks][w] = sign == 0.0f ? 0u : qf[ks][w] ^ 0x80008000u;
+          }
+        }
+      }
+    }
+    f32x16 acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    const int64_t head0 = (int64_t)h * head_bytes;
+    const int page_keys = kPageCap << a.ps_shift;
+    const int seg_tiles = max(1, page_keys / C::TK);
+    for (int t0 = k0; t0 < k1; t0 += seg_tiles) {
+      const int t1 = min(k1, t0 + seg_tiles);
+      // ---- page indices of the segment's keys, checked
+      const int pg0 = (t0 * C::TK) >> a.ps_shift;
+      __syncthreads();
+      {
+        const int last = (min(t1 * C::TK, s.len) - 1) >> a.ps_shift;
+        for (int i = tid; i < kPageCap; i += C::WAVES * 64) {
+          int pg = -1;
+          if (pg0 + i <= last) {
+            pg = a.table[(int64_t)b * a.max_pages + pg0 + i];
+            if ((uint32_t)pg >= (uint32_t)a.n_pages) {
+              pg = -1;
+              bad = RLK_DERR_PAGE;
+            }
+          }
+          s_pages[i] = pg;
+        }
+      }
+      __syncthreads();
+
+      // ---- copies of this wavefront's rows of a tile into a stage
+      auto copy_tile = [&](int t, int stage) {
+        if (t >= t1) t = t1 - 1;  // keeps the count of copies in flight; nobody reads it
+        const int part0 = t * C::TK + kw * C::PK + wm * C::LROWS;  // first key of the share
+        char* dst = smem + stage * C::STAGE + kw * C::PART + wm * C::LROWS * G::ROWB;
+        if (paged_rows) {
+          // page of each copy, one lane each
+          const int kk = part0 + (lane < NI ? lane : 0) * G::RPI;
+          const int pv = s_pages[min((kk >> a.ps_shift) - pg0, kPageCap - 1)];
+#pragma unroll NI <= 4 ? NI : 2
+          for (int i = 0; i < NI; ++i) {
+            const int key = part0 + i * G::RPI;
+            const int pg = __builtin_amdgcn_readlane(pv, i);
+            const int in = key & ((1 << a.ps_shift) - 1);
+            const int rows = min((1 << a.ps_shift) - in, s.len - key);  // rows from here on in the page and the sequence
+            const uint32_t size = pg >= 0 && rows > 0 ? (uint32_t)rows * (uint32_t)row_bytes : 0u;
+            const int64_t at = pg >= 0 ? pg * page_bytes + head0 + in * row_bytes : 0;
+            const int lr = wm * C::LROWS + i * G::RPI + crow;
+            const int ck = cchunk ^ G::k_swz(lr), cv = cchunk ^ G::v_swz(lr);
+            const uint32_t ro = crow * (uint32_t)row_bytes;
+            const uint32_t ok = ck * EPC < a.D ? ro + ck * 16 : 0x80000000u;
+            const uint32_t ov = cv * EPC < a.D ? ro + cv * 16 : 0x80000000u;
+            const __amdgpu_buffer_rsrc_t rk =
+                __builtin_amdgcn_make_buffer_rsrc((char*)a.k_pages + at, (short)0, (int)size, 0x00020000);
+            const __amdgpu_buffer_rsrc_t rv =
+                __builtin_amdgcn_make_buffer_rsrc((char*)a.v_pages + at, (short)0, (int)size, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, LDSP(dst + i * 1024), 16, ok, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, LDSP(dst + C::WK * C::PART + i * 1024), 16, ov, 0, 0, 0);
+          }
+        } else {
+          // pages smaller than a copy's rows: every lane finds its own; rows behind the sequence repeat its last
+          const int nch = a.D / EPC;
+#pragma unroll 1
+          for (int i = 0; i < NI; ++i) {
+            const int key = min(part0 + i * G::RPI + crow, s.len - 1);
+            const int pg = max(s_pages[min((key >> a.ps_shift) - pg0, kPageCap - 1)], 0);
+            const int64_t at = pg * page_bytes + head0 + (key & ((1 << a.ps_shift) - 1)) * row_bytes;
+            const int lr = wm * C::LROWS + i * G::RPI + crow;
+            int ck = cchunk ^ G::k_swz(lr), cv = cchunk ^ G::v_swz(lr);
+            if (ck >= nch) ck %= nch;  // columns behind the head: the query's are 0, the output's not stored
+            if (cv >= nch) cv %= nch;
+            if (a.n_pages > 0) {
+              __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((char*)a.k_pages + at + ck * 16),
+                                               LDSP(dst + i * 1024), 16, 0, 0);
+              __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((char*)a.v_pages + at + cv * 16),
+                                               LDSP(dst + C::WK * C::PART + i * 1024), 16, 0, 0);
+            }
+          }
+        }
+        if (p.slot_end && lane < C::PK) {
+          // the same for every wavefront of a row split: each waits for its own copy
+          const int key = min(t * C::TK + kw * C::PK + lane, s.len - 1);
+          __builtin_amdgcn_global_load_lds(
+              (const __attribute__((address_space(1))) void*)(p.slot_end + (int64_t)b * p.end_stride + key),
+              LDSP(s_ends + stage * C::TK + kw * C::PK), 4, 0, 0);
+        }
+      };
+
+      wait_vmcnt<0>();  // the counts below are of copies alone
+#pragma unroll
+      for (int st = 0; st < NS - 1; ++st) copy_tile(t0 + st, st);
+      int stage = 0;
+      for (int t = t0; t < t1; ++t) {
+        const int part0 = t * C::TK + kw * C::PK;
+        // the tile that falls NS - 1 further goes where the last one was read; then wait for this one
+        if constexpr (C::WM == 1) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          copy_tile(t + NS - 1, stage == 0 ? NS - 1 : stage - 1);
+          if (p.slot_end) wait_vmcnt<(NS - 1) * (2 * NI + 1)>();
+          else wait_vmcnt<(NS - 1) * 2 * NI>();
+        } else {
+          if (p.slot_end) wait_vmcnt<(NS - 2) * (2 * NI + 1)>();
+          else wait_vmcnt<(NS - 2) * 2 * NI>();
+        }
+        // A part that some row does not see whole: masked, and its values are looked through for NaN and infinities,
+        // which a zero probability does not keep out of a product.
+        const bool masked = part0 + C::PK - 1 > (C::WM == 1 ? first_slot : ctx + tok0) || p.slot_end != nullptr;
+        const char* kst = smem + stage * C::STAGE;
+        if (masked) {
+          uint32_t odd = 0;
+          const char* v0 = kst + (C::WK + kw) * C::PART + wm * C::LROWS * G::ROWB + lane * 16;
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(v0 + i * 1024);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              if constexpr (ESZ == 2) odd |= ((v[w] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+              else odd |= ((v[w] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+            }
+          }
+          const bool any = __any(odd != 0);
+          if (lane == 0) s_flag[stage * 8 + wid] = any;
+        }
+        if constexpr (C::WM > 1) {
+          block_barrier();
+          copy_tile(t + NS - 1, stage == 0 ? NS - 1 : stage - 1);
+        }
+        if (part0 <= last_slot) {
+          // ---- scores
+          f32x16 sc[NB];
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[nb][r] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < CPR / 2; ++ks) {
+              const u32x4 kf = *reinterpret_cast<const u32x4*>(kst + ((k_base + nb * 32 * G::ROWB) ^ (ks << 5)));
+              if constexpr (ESZ == 2) {
+                sc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+                                                                 __builtin_bit_cast(bf16x8, qf[ks]), sc[nb], 0, 0, 0);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  sc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qf[ks][e]), sc[nb], 0,
+                                                                0, 0);
+              }
+            }
+          }
+          bool poisoned = false;
+          if (masked) {
+            int any = 0;
+#pragma unroll
+            for (int w = 0; w < C::WM; ++w) any |= s_flag[stage * 8 + (C::WM > 1 ? w : wid)];
+            poisoned = __builtin_amdgcn_readfirstlane(any) != 0;
+            const int rel = qslot - part0 - 4 * hl;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) sc[nb][r] = nb * 32 + key_of(r, 0) > rel ? -INFINITY : sc[nb][r];
+            if (p.slot_end) {
+              const int* ends = s_ends + stage * C::TK + kw * C::PK + 4 * hl;
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                  const u32x4 e = *reinterpret_cast<const u32x4*>(ends + nb * 32 + 2 * r);
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) sc[nb][r + i] = (int)e[i] <= qslot ? -INFINITY : sc[nb][r + i];
+                }
+            }
+          }
+          // ---- running maximum and sum
+          float mx = sc[0][0];
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[nb][r]);
+          mx = swap_max(mx);
+          if (__any((mx - m) * c > kLazy || (m == -INFINITY && mx > m))) {
+            const float m2 = fmaxf(m, mx);
+            const float al = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - m2) * c);
+            l *= al;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) acc[d][r] *= al;
+            m = m2;
+          }
+          const float mb = m == -INFINITY ? 0.0f : m * c;
+          float sum = 0.0f;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              sc[nb][r] = __builtin_amdgcn_exp2f(fmaf(sc[nb][r], c, -mb));
+              sum += sc[nb][r];
+            }
+          l += sum;
+          // ---- values
+          if constexpr (ESZ == 2) {
+            int u[VB];
+#pragma unroll
+            for (int d = 0; d < VB; ++d) u[d] = v_base[d] + stage * C::STAGE;
+            auto step = [&](auto NBK, auto SK) {
+              constexpr int nb = decltype(NBK)::value, sk = decltype(SK)::value;
+              u32x4 pf;
+#pragma unroll
+              for (int w = 0; w < 4; ++w) pf[w] = pack_bf16x2(sc[nb][sk * 8 + 2 * w], sc[nb][sk * 8 + 2 * w + 1]);
+              constexpr int off = (nb * 32 + sk * 16) * G::ROWB;
+              auto blocks = [&](auto D0) {
+                constexpr int d0 = decltype(D0)::value;
+                u32x4 vf[VB];
+                read_v<VB, off + d0 * 64, 8 * G::ROWB>(u, vf);
+                if (poisoned) {
+                  u32x4 ind;
+#pragma unroll
+                  for (int w = 0; w < 4; ++w)
+                    ind[w] = (sc[nb][sk * 8 + 2 * w] > 0.0f ? 0x3f80u : 0u) | (sc[nb][sk * 8 + 2 * w + 1] > 0.0f ? 0x3f800000u : 0u);
+#pragma unroll
+                  for (int d = 0; d < VB; ++d) {
+                    u32x4 up, down;
+                    take_nonfinite(vf[d], up, down);
+                    f32x16 t = {};
+                    t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, ind),
+                                                                t, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[d0 + d][r] += t[r] > 0.0f ? INFINITY : 0.0f;
+                    t = f32x16{};
+                    t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, down),
+                                                                __builtin_bit_cast(bf16x8, ind), t, 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[d0 + d][r] -= t[r] > 0.0f ? INFINITY : 0.0f;
+                  }
+                }
+#pragma unroll
+                for (int d = 0; d < VB; ++d)
+                  acc[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]),
+                                                                        __builtin_bit_cast(bf16x8, pf), acc[d0 + d], 0, 0, 0);
+              };
+              blocks(std::integral_constant<int, 0>{});
+              if constexpr (DB > 4) blocks(std::integral_constant<int, 4>{});
+            };
+            step(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+            step(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
+            if constexpr (NB > 1) {
+              step(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{});
+              step(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
+            }
+          } else {
+            const char* v0 = kst + (C::WK + kw) * C::PART;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const int k = nb * 32 + key_of(r, 0);  // half 1: 4 rows on
+                const int rowb = (k + 4 * hl) * G::ROWB;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                  const int chunk = (d * 8 + (ql >> 2)) ^ (((k + 4 * hl) & 4) << 1);
+                  float v = *reinterpret_cast<const float*>(v0 + rowb + chunk * 16 + (ql & 3) * 4);
+                  if (poisoned) {
+                    const float ind = sc[nb][r] > 0.0f ? 1.0f : 0.0f;
+                    const bool odd = !(fabsf(v) < INFINITY);
+                    f32x16 t = {};
+                    t = __builtin_amdgcn_mfma_f32_32x32x2f32(odd && !(v < 0.0f) ? 1.0f : 0.0f, ind, t, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[d][i] += t[i] > 0.0f ? INFINITY : 0.0f;
+                    t = f32x16{};
+                    t = __builtin_amdgcn_mfma_f32_32x32x2f32(odd && !(v > 0.0f) ? 1.0f : 0.0f, ind, t, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[d][i] -= t[i] > 0.0f ? INFINITY : 0.0f;
+                    v = odd ? 0.0f : v;
+                  }
+                  acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[nb][r], acc[d], 0, 0, 0);
+                }
+              }
+          }
+        }
+        stage = stage + 1 == NS ? 0 : stage + 1;
+      }
+      wait_vmcnt<0>();
+    }
+
+    // ---- the tile's result: outputs, or a part of them
+    l = swap_sum(l);
+    float big = m == -INFINITY ? -INFINITY : m * c;  // in powers of 2
+    const int slot = x0 > 0 ? 2 * wg : 2 * wg + 1;
+    float* po = pl.part + (int64_t)slot * C::BM * DP;
+    float2* pml = pl.ml + (int64_t)slot * C::BM;
+    if constexpr (C::WK > 1) {
+      float* jo = reinterpret_cast<float*>(smem);
+      float2* jm = reinterpret_cast<float2*>(smem + C::WK * 32 * C::OROW * 4);
+      __syncthreads();
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<f32x4*>(jo + (kw * 32 + ql) * C::OROW + d * 32 + key_of(r, hl)) =
+              f32x4{acc[d][r], acc[d][r + 1], acc[d][r + 2], acc[d][r + 3]};
+      if (hl == 0) jm[kw * 32 + ql] = make_float2(big, l);
+      __syncthreads();
+      constexpr int LPR = C::WAVES * 64 / 32;  // lanes of a row
+      const int jr = tid / LPR, jl = tid % LPR;
+      float M = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < C::WK; ++k) M = fmaxf(M, jm[k * 32 + jr].x);
+      float f[C::WK], L = 0.0f;
+#pragma unroll
+      for (int k = 0; k < C::WK; ++k) {
+        const float2 ml = jm[k * 32 + jr];
+        f[k] = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - M);
+        L += ml.y * f[k];
+      }
+      const int jt = jr / g;
+      if (jt < ntok) {
+        const int64_t t = s.row0 + tok0 + jt, qh = h * g + jr % g;
+        const float inv = L > 0.0f ? 1.0f / L : (L == 0.0f ? 0.0f : L);
+        for (int e = jl * 4; e < a.D; e += LPR * 4) {
+          f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+          for (int k = 0; k < C::WK; ++k) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(jo + (k * 32 + jr) * C::OROW + e);
+            if (f[k] != 0.0f) o += v * f[k];
+          }
+          if (whole) {
+            o *= inv;
+            T* dst = (T*)p.out + (t * a.Hq + qh) * a.D + e;
+            if constexpr (ESZ == 2) *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+            else *reinterpret_cast<f32x4*>(dst) = o;
+          } else {
+            *reinterpret_cast<f32x4*>(po + jr * DP + e) = o;
+          }
+        }
+        if (jl == 0) {
+          if (!whole) pml[jr] = make_float2(M, L);
+          else if (p.lse) p.lse[t * a.Hq + qh] = L == 0.0f ? -INFINITY : M * kLn2f + logf(L);
+        }
+      }
+      __syncthreads();
+    } else if (live) {
+      const int64_t t = s.row0 + tok0 + rtok, qh = h * g + row % g;
+      const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int e = d * 32 + key_of(r, hl);
+          if (e >= a.D) continue;
+          f32x4 o = {acc[d][r], acc[d][r + 1], acc[d][r + 2], acc[d][r + 3]};
+          if (whole) {
+            o *= inv;
+            T* dst = (T*)p.out + (t * a.Hq + qh) * a.D + e;
+            if constexpr (ESZ == 2) *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+            else *reinterpret_cast<f32x4*>(dst) = o;
+          } else {
+            *reinterpret_cast<f32x4*>(po + (int64_t)row * DP + e) = o;
+          }
+        }
+      if (hl == 0) {
+        if (!whole) pml[row] = make_float2(big, l);
+        else if (p.lse) p.lse[t * a.Hq + qh] = l == 0.0f ? -INFINITY : big * kLn2f + logf(l);
+      }
+    }
+    if (x0 == 0 && x1 < cost) md = {b, h, rt, (int)((start + cost - 1) / piece)};
+
+    // ---- next item
+    start += cost;
+    if (start >= hi) break;
+    ++rt;
+    if (rt * tpt >= s.n) {
+      rt = 0;
+      do {
+        if (++b == a.B) {
+          b = 0;
+          ++h;
+        }
+        s = sequence(a, b);
+      } while (s.n == 0);
+    }
+  }
+  if (tid == 0) *desc = md;
+  const int wg_bad = __syncthreads_or(bad);
+  if (tid == 0) pl.flags[wg] = wg_bad ? RLK_DERR_PAGE : 0;
+}
+
+// Joins the parts of a row tile that was cut between workgroups: workgroup (x, y) rows y * 256 / (DP / 4) of the tile
+// that workgroup x of the attention began and did not end.  The last workgroup in x makes the status word.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256) k_kv_merge(KvArgs a, AttnArgs p, AttnPlan pl, int BM) {
+  constexpr int LPR = DP / 4, RPB = 256 / LPR;
+  const int w = blockIdx.x, tid = threadIdx.x;
+  if (w == (int)gridDim.x - 1) {
+    if (blockIdx.y != 0) return;
+    int bad = tid == 0 && a.cu[0] != 0 ? RLK_DERR_CU_SEQLENS : 0;
+    for (int b = tid; b < a.B; b += 256) sequence(a, b, &bad);
+    for (int i = tid; i < w; i += 256) bad |= pl.flags[i];
+    __shared__ int s_bad;
+    if (tid == 0) s_bad = 0;
+    __syncthreads();
+    if (bad) atomicOr(&s_bad, bad);
+    __syncthreads();
+    if (tid == 0) *pl.status = s_bad;
+    return;
+  }
+  const MergeDesc d = pl.desc[w];
+  if (d.last < 0) return;
+  const Seq s = sequence(a, d.b);
+  const int g = a.Hq / a.Hkv, row = blockIdx.y * RPB + tid / LPR, e = (tid % LPR) * 4;
+  const int tok = d.rt * pl.tpt + row / g;
+  if (row >= BM || row / g >= pl.tpt || tok >= s.n) return;
+  float M = -INFINITY;
+  for (int k = w; k <= d.last; ++k) M = fmaxf(M, pl.ml[(int64_t)(k == w ? 2 * k + 1 : 2 * k) * BM + row].x);
+  float L = 0.0f;
+  f32x4 o = {0, 0, 0, 0};
+  for (int k = w; k <= d.last; ++k) {
+    const int64_t at = (int64_t)(k == w ? 2 * k + 1 : 2 * k) * BM + row;
+    const float2 ml = pl.ml[at];
+    if (ml.x == -INFINITY && ml.y == 0.0f) continue;
+    const float f = __builtin_amdgcn_exp2f(ml.x - M);
+    L += ml.y * f;
+    if (e < a.D) o += *reinterpret_cast<const f32x4*>(pl.part + at * DP + e) * f;
+  }
+  const int64_t t = s.row0 + tok, qh = d.h * g + row % g;
+  const float inv = L > 0.0f ? 1.0f / L : (L == 0.0f ? 0.0f : L);
+  if (e < a.D) {
+    o *= inv;
+    T* dst = (T*)p.out + (t * a.Hq + qh) * a.D + e;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+    else *reinterpret_cast<f32x4*>(dst) = o;
+  }
+  if (e == 0 && p.lse) p.lse[t * a.Hq + qh] = L == 0.0f ? -INFINITY : M * kLn2f + logf(L);
+}
+
+// Tiles by type and head size.  Few: 32 query rows, the wavefronts split the keys (one to a few tokens: bound by the
+// cache's bytes).  Many: 128 rows, 32 to a wavefront.
+template <typename T, int DP> struct Few;
+template <typename T, int DP> struct Many;
+template <> struct Few<bf16_t, 64> : Cfg<bf16_t, 64, 1, 4, 1, 4> {};
+template <> struct Few<bf16_t, 128> : Cfg<bf16_t, 128, 1, 4, 1, 2> {};
+template <> struct Few<bf16_t, 256> : Cfg<bf16_t, 256, 1, 2, 1, 2> {};
+template <> struct Few<float, 64> : Cfg<float, 64, 1, 4, 1, 2> {};
+template <> struct Few<float, 128> : Cfg<float, 128, 1, 2, 1, 2> {};
+template <> struct Few<float, 256> : Cfg<float, 256, 1, 1, 1, 2> {};
+template <> struct Many<bf16_t, 64> : Cfg<bf16_t, 64, 4, 1, 2, 3> {};
+template <> struct Many<bf16_t, 128> : Cfg<bf16_t, 128, 4, 1, 2, 2> {};
+template <> struct Many<bf16_t, 256> : Cfg<bf16_t, 256, 4, 1, 1, 2> {};
+template <> struct Many<float, 64> : Cfg<float, 64, 4, 1, 1, 2> {};
+template <> struct Many<float, 128> : Cfg<float, 128, 4, 1, 1, 2> {};
+template <> struct Many<float, 256> : Cfg<float, 256, 4, 1, 1, 2> {};
+
+constexpr int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+// What the launch and the workspace share.
+struct Shape {
+  bool few;
+  int DP, BM, tpt, wgs;
+};
+Shape shape(const KvArgs& a, int max_new) {
+  Shape s;
+  const int g = a.Hq / a.Hkv;
+  const int64_t most = max_new > 0 ? std::min<int64_t>(max_new, a.T) : a.T;
+  s.DP = padded_dim(a.D);
+  s.few = g <= 32 && most * g <= 32;
+  s.BM = s.few ? 32 : 128;
+  s.tpt = s.BM / g;
+  s.wgs = s.few ? 256 : 512;
+  return s;
+}
+
+template <typename T, typename C>
+hipError_t run(const KvArgs& a, const AttnArgs& p, const AttnPlan& pl, int wgs, hipStream_t s) {
+  static std::once_flag once[64];
+  static hipError_t err[64];
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess || dev < 0 || dev >= 64) return e != hipSuccess ? e : hipErrorInvalidDevice;
+  std::call_once(once[dev], [&] {
+    err[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_kv_attn<T, C>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   C::LDS);
+  });
+  if (err[dev] != hipSuccess) return err[dev];
+  k_kv_attn<T, C><<<wgs, C::WAVES * 64, C::LDS, s>>>(a, p, pl);
+  constexpr int rows = 256 / (C::DP / 4);
+  k_kv_merge<T, C::DP><<<dim3(wgs + 1, (C::BM + rows - 1) / rows), 256, 0, s>>>(a, p, pl, C::BM);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_type(const Shape& sh, const KvArgs& a, const AttnArgs& p, const AttnPlan& pl, hipStream_t s) {
+  if (sh.DP == 64) return sh.few ? run<T, Few<T, 64>>(a, p, pl, sh.wgs, s) : run<T, Many<T, 64>>(a, p, pl, sh.wgs, s);
+  if (sh.DP == 128) return sh.few ? run<T, Few<T, 128>>(a, p, pl, sh.wgs, s) : run<T, Many<T, 128>>(a, p, pl, sh.wgs, s);
+  return sh.few ? run<T, Few<T, 256>>(a, p, pl, sh.wgs, s) : run<T, Many<T, 256>>(a, p, pl, sh.wgs, s);
+}
+
+constexpr size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+struct Layout {
+  size_t desc, flags, ml, part, total;
+};
+// of the larger of the two shapes: the size does not depend on max_new
+Layout layout(int DP, int wgs, int BM) {
+  Layout L;
+  size_t o = up256(sizeof(WsHeader));
+  L.desc = o;
+  o += up256((size_t)wgs * sizeof(MergeDesc));
+  L.flags = o;
+  o += up256((size_t)wgs * 4);
+  L.ml = o;
+  o += up256((size_t)wgs * 2 * BM * 8);
+  L.part = o;
+  o += (size_t)wgs * 2 * BM * DP * 4;
+  L.total = o;
+  return L;
+}
+
+}  // namespace
+
+size_t kv_attention_workspace(int D) { return layout(padded_dim(D), 512, 128).total; }
+
+hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, int max_new, char* ws, hipStream_t s) {
+  prof_mark(KK_KV_ATTENTION, true, s);
+  const Shape sh = shape(a, max_new);
+  const Layout L = layout(sh.DP, sh.wgs, sh.BM);
+  AttnPlan pl = {};
+  pl.tpt = sh.tpt;
+  pl.min_piece = 512;
+  pl.desc = reinterpret_cast<MergeDesc*>(ws + L.desc);
+  pl.flags = reinterpret_cast<int32_t*>(ws + L.flags);
+  pl.ml = reinterpret_cast<float2*>(ws + L.ml);
+  pl.part = reinterpret_cast<float*>(ws + L.part);
+  pl.status = &reinterpret_cast<WsHeader*>(ws)->status;
+  const hipError_t e = dtype == RLK_DTYPE_BF16 ? run_type<bf16_t>(sh, a, p, pl, s) : run_type<float>(sh, a, p, pl, s);
+  prof_mark(KK_KV_ATTENTION, false, s);
+  return e;
+}
+
+}  // namespace rlk

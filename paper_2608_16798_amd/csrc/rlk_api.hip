@@ -1116,7 +1116,7 @@ rlk_status_t rlk_kv_workspace_size(const rlk_kv_t* c, size_t* bytes) {
   if (!bytes) return fail(RLK_EINVAL, "bytes is NULL");
   rlk_status_t st = check_kv(c);
   if (st) return st;
-  *bytes = align256(sizeof(WsHeader));
+  *bytes = kv_attention_workspace(c->head_dim);
   return RLK_OK;
 }
 
@@ -1208,7 +1208,7 @@ rlk_status_t rlk_kv_attention(const rlk_kv_t* c, const void* q, int64_t q_stride
   a.scale = scale;
   a.out = out;
   a.lse = lse;
-  RLK_TRY(launch_kv_attention(c->dtype, k, a, &static_cast<WsHeader*>(ws)->status, s), "kv_attention");
+  RLK_TRY(launch_kv_attention(c->dtype, k, a, c->max_new, static_cast<char*>(ws), s), "kv_attention");
   return finish(hipSuccess, "", ws, s);
 }
 

@@ -306,7 +306,9 @@ struct AttnArgs {
   void* out;
   float* lse;  // may be NULL
 };
-hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, int32_t* status, hipStream_t s);
+// ---- launchers (k_kv_attn.hip) ----
+size_t kv_attention_workspace(int D);  // header first
+hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, int max_new, char* ws, hipStream_t s);
 
 // ---- launchers (k_verify.hip) ----
 struct VerifyArgs {
