@@ -8,7 +8,10 @@
 //   3. draw: the chunk that holds the target, then the token in it.
 #include "rlk_internal.h"
 
+#include <limits.h>
 #include <math.h>
+
+#include <algorithm>
 
 namespace rlk {
 
@@ -59,29 +62,35 @@ __device__ __forceinline__ float load_logit(const T* row, int i) {
   else return row[i];
 }
 
-// 2^t for t <= 0 (0 below -1,100), to about 1e-14 of its value: whole part by the exponent, 2^f on [-1/2, 1/2] by the
-// exponential series of f ln 2 up to the eleventh power (the twelfth is below 7e-15).
+// 2^t for t <= 0, to 2e-14 of its value; 2^-1000 below that.  The nearest whole number n comes out of the sum with
+// 1.5 2^52 (its low word), 2^f for the rest f in [-1/2, 1/2] out of the polynomial through the ten Chebyshev nodes of that
+// interval, and n goes into the exponent: fifteen fp64 operations, of which the whole pass is made.
 __device__ __forceinline__ double pow2(double t) {
-  t = fmax(t, -1100.0);
-  const double n = rint(t), y = (t - n) * 0.69314718055994530942;
-  double p = 1.0 / 39916800.0;
-  p = fma(p, y, 1.0 / 3628800.0);
-  p = fma(p, y, 1.0 / 362880.0);
-  p = fma(p, y, 1.0 / 40320.0);
-  p = fma(p, y, 1.0 / 5040.0);
-  p = fma(p, y, 1.0 / 720.0);
-  p = fma(p, y, 1.0 / 120.0);
-  p = fma(p, y, 1.0 / 24.0);
-  p = fma(p, y, 1.0 / 6.0);
-  p = fma(p, y, 0.5);
-  p = fma(p, y, 1.0);
-  p = fma(p, y, 1.0);
-  return ldexp(p, (int)n);
+  t = fmax(t, -1000.0);
+  const double u = t + 6755399441055744.0, f = t - (u - 6755399441055744.0);
+  double p = 1.0205905413765595e-07;
+  p = fma(p, f, 1.325964524488711e-06);
+  p = fma(p, f, 1.5252672924850737e-05);
+  p = fma(p, f, 0.0001540343375125101);
+  p = fma(p, f, 0.0013333558200794592);
+  p = fma(p, f, 0.009618129193934313);
+  p = fma(p, f, 0.05550410866465167);
+  p = fma(p, f, 0.2402265069564034);
+  p = fma(p, f, 0.6931471805599462);
+  p = fma(p, f, 1.0000000000000135);
+  return __hiloint2double(__double2hiint(p) + (int)((uint32_t)__double2loint(u) << 20), __double2loint(p));
 }
 
-// exp((z - m) / tau) with c = log2(e) / tau; 0 for z = -inf and wherever m is -inf (a chunk without mass)
-__device__ __forceinline__ double weight(float z, double m, double c) {
-  return m == -INFINITY ? 0.0 : pow2(((double)z - m) * c);
+// exp((z - m) / tau) with c = log2(e) / tau and b = -m c, the largest logit m finite
+__device__ __forceinline__ double weight(float z, double c, double b) { return pow2(fma((double)z, c, b)); }
+// the same, exactly 0 where there is no mass
+__device__ __forceinline__ double mass_of(float z, double c, double b) {
+  const double t = fma((double)z, c, b);
+  return t < -999.0 ? 0.0 : pow2(t);
+}
+// a chunk's sum against the row's largest logit
+__device__ __forceinline__ double rescaled(double s, double m, double row_m, double c) {
+  return m == -INFINITY ? s : s * pow2((m - row_m) * c);
 }
 
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -100,7 +109,7 @@ __global__ void __launch_bounds__(256) k_verify_stats(VerifyArgs a, Part* part, 
   const T* z = row < rows ? (const T*)a.logits + row * a.ld_logits : (const T*)a.draft_logits + (row - rows) * a.ld_draft;
   float x[I][E];
   float m = -INFINITY;
-  bool nan = false;
+  uint32_t top = 0;  // largest magnitude by its bits: above those of infinity, a NaN
 #pragma unroll
   for (int i = 0; i < I; ++i) load_logits(z, c * kChunk + (i * 256 + (int)threadIdx.x) * E, a.V, x[i]);
 #pragma unroll
@@ -108,7 +117,7 @@ __global__ void __launch_bounds__(256) k_verify_stats(VerifyArgs a, Part* part, 
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       m = fmaxf(m, x[i][e]);
-      nan |= !(x[i][e] < INFINITY);
+      top = max(top, __float_as_uint(x[i][e]) & 0x7fffffffu);
     }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
@@ -119,11 +128,14 @@ __global__ void __launch_bounds__(256) k_verify_stats(VerifyArgs a, Part* part, 
   __syncthreads();
   m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
   double s = 0.0;
+  if (m > -INFINITY && m < INFINITY) {
+    const double b = -(double)m * a.c;
 #pragma unroll
-  for (int i = 0; i < I; ++i)
+    for (int i = 0; i < I; ++i)
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += weight(x[i][e], m, a.c);
-  if (nan) s = NAN;
+      for (int e = 0; e < E; ++e) s += weight(x[i][e], a.c, b);
+  }
+  if (top > 0x7f800000u || m == INFINITY) s = NAN;
   s = wave_sum64(s);
   if ((threadIdx.x & 63) == 0) s_s[w] = s;
   __syncthreads();
@@ -140,7 +152,7 @@ __device__ __forceinline__ Part row_total(const Part* part, int nchunk, double c
   double s = 0.0;
   for (int i = lane; i < nchunk; i += 64) {
     const Part p = part[i];
-    s += p.m == -INFINITY ? p.s : p.s * pow2((p.m - m) * c);
+    s += rescaled(p.s, p.m, m, c);
   }
   return {wave_sum64(s), m};
 }
@@ -163,7 +175,7 @@ struct Choice {
 
 template <typename T>
 __global__ void __launch_bounds__(256) k_verify_decide(VerifyArgs a, const Part* part, double* mass, Choice* choice,
-                                                       int32_t* status) {
+                                                       int per, int32_t* status) {
   constexpr int E = 16 / (int)sizeof(T), I = kChunk / (256 * E);
   const int c = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, w = tid >> 6;
   __shared__ Part s_p[4], s_q[4];
@@ -196,9 +208,9 @@ __global__ void __launch_bounds__(256) k_verify_decide(VerifyArgs a, const Part*
           if (a.draft_logits) {
             q = row_total(part + (rows + sp.d0 + i) * a.nchunk, a.nchunk, a.c);
             if (!(q.s > 0.0 && q.m < INFINITY)) wrong |= RLK_DERR_LOGITS;
-            qy = weight(load_logit((const T*)a.draft_logits + (sp.d0 + i) * a.ld_draft, y), q.m, a.c) / q.s;
+            qy = mass_of(load_logit((const T*)a.draft_logits + (sp.d0 + i) * a.ld_draft, y), a.c, -q.m * a.c) / q.s;
           }
-          const double py = weight(load_logit((const T*)a.logits + (r0 + i) * a.ld_logits, y), p.m, a.c) / p.s;
+          const double py = mass_of(load_logit((const T*)a.logits + (r0 + i) * a.ld_logits, y), a.c, -p.m * a.c) / p.s;
           ok = (double)a.u_accept[sp.d0 + i] * qy < py;
         }
       }
@@ -247,138 +259,162 @@ __global__ void __launch_bounds__(256) k_verify_decide(VerifyArgs a, const Part*
     }
   }
   if (bad) return;
-  // this chunk's mass of the row that the token is drawn from
-  const Part mine = part[(r0 + acc) * a.nchunk + c];
-  const double as_p = mine.m == -INFINITY ? 0.0 : mine.s * pow2((mine.m - p.m) * a.c) / p.s;
+  // the masses, of this workgroup's chunks, of the row that the token is drawn from
   const int y = residual ? a.draft[sp.d0 + acc] : -1;
-  if (!residual || (!a.draft_logits && y / kChunk != c)) {
-    if (tid == 0) mass[(int64_t)b * a.nchunk + c] = as_p;
-    return;
-  }
-  double sum = 0.0;
   const T* zp = (const T*)a.logits + (r0 + acc) * a.ld_logits;
-  const T* zq = a.draft_logits ? (const T*)a.draft_logits + (sp.d0 + acc) * a.ld_draft : nullptr;
-#pragma unroll
-  for (int i = 0; i < I; ++i) {
-    const int at = c * kChunk + (i * 256 + tid) * E;
-    float x[E], xq[E];
-    load_logits(zp, at, a.V, x);
-    if (zq) load_logits(zq, at, a.V, xq);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const double v = weight(x[e], p.m, a.c) / p.s;
-      if (zq) sum += fmax(v - weight(xq[e], q.m, a.c) / q.s, 0.0);
-      else sum += at + e == y ? 0.0 : v;
+  const T* zq = residual && a.draft_logits ? (const T*)a.draft_logits + (sp.d0 + acc) * a.ld_draft : nullptr;
+  const double bp = -p.m * a.c, bq = -q.m * a.c, np = 1.0 / p.s, nq = 1.0 / q.s;
+  for (int ch = c * per; ch < min(a.nchunk, (c + 1) * per); ++ch) {
+    if (!residual || (!zq && y / kChunk != ch)) {
+      const Part mine = part[(r0 + acc) * a.nchunk + ch];
+      if (tid == 0) mass[(int64_t)b * a.nchunk + ch] = rescaled(mine.s, mine.m, p.m, a.c) * np;
+      continue;
     }
+    float x[I][E], xq[I][E];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      load_logits(zp, ch * kChunk + (i * 256 + tid) * E, a.V, x[i]);
+      if (zq) load_logits(zq, ch * kChunk + (i * 256 + tid) * E, a.V, xq[i]);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const double v = mass_of(x[i][e], a.c, bp) * np;
+        if (zq) sum += fmax(v - mass_of(xq[i][e], a.c, bq) * nq, 0.0);
+        else sum += ch * kChunk + (i * 256 + tid) * E + e == y ? 0.0 : v;
+      }
+    sum = wave_sum64(sum);
+    __syncthreads();
+    if ((tid & 63) == 0) s_sum[w] = sum;
+    __syncthreads();
+    if (tid == 0) mass[(int64_t)b * a.nchunk + ch] = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
   }
-  sum = wave_sum64(sum);
-  if ((tid & 63) == 0) s_sum[w] = sum;
-  __syncthreads();
-  if (tid == 0) mass[(int64_t)b * a.nchunk + c] = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
 }
 
-// Inclusive sum over the workgroup's 256 threads; *total gets the whole.
-__device__ __forceinline__ double block_scan(double v, double* s_w, double* total) {
+// N inclusive sums over the workgroup's 256 threads at once, each behind the one before it: v[i] becomes the sum over
+// the whole of v[0 .. i - 1] and the threads up to this one of v[i].  Returns the whole.
+template <int N>
+__device__ __forceinline__ double block_scan(double (&v)[N], double (*s_w)[4]) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
+  for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const double u = __shfl_up(v[i], o, 64);
+      if (lane >= o) v[i] += u;
+    }
   __syncthreads();
-  if (lane == 63) s_w[w] = v;
+  if (lane == 63)
+#pragma unroll
+    for (int i = 0; i < N; ++i) s_w[i][w] = v[i];
   __syncthreads();
-  double before = 0.0;
-  for (int k = 0; k < w; ++k) before += s_w[k];
-  *total = s_w[0] + s_w[1] + s_w[2] + s_w[3];
-  return before + v;
+  double base = 0.0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k == w) v[i] += base;
+      base += s_w[i][k];
+    }
+  return base;
 }
 
-// Smallest index that passes the target, over the workgroup: s_best holds INT_MAX before.
+// One workgroup per sequence: the chunk whose running mass passes the target, then the token in it.
 template <typename T>
 __global__ void __launch_bounds__(256) k_verify_draw(VerifyArgs a, const Part* part, const double* mass,
                                                      const Choice* choice) {
   constexpr int E = 16 / (int)sizeof(T), I = kChunk / (256 * E);
+  constexpr int M = (RLK_MAX_DIM / kChunk + 255) / 256;  // most chunks of a thread
   const int b = blockIdx.x, tid = threadIdx.x;
   const Choice ch = choice[b];
   if (ch.acc < 0) return;
-  __shared__ double s_w[4];
-  __shared__ int s_first, s_last;
+  __shared__ double s_w[I > M ? I : M][4];
+  __shared__ int s_first, s_last, s_pick, s_any;
   __shared__ double s_before;
   const int64_t d0 = a.cu[b], r0 = d0 + b;
   const double* mb = mass + (int64_t)b * a.nchunk;
   const Part* pb = part + (r0 + ch.acc) * a.nchunk;
-  // A residual of nothing (p and q the same, and the comparison fell to rounding): drawn from p.
   bool residual = ch.residual != 0;
-  double total = 0.0;
-  for (int c = 0; c < a.nchunk; ++c) total += mb[c];
-  if (residual && !(total > 0.0)) {
-    residual = false;
-    total = 0.0;
-    for (int c = 0; c < a.nchunk; ++c) total += pb[c].m == -INFINITY ? 0.0 : pb[c].s * pow2((pb[c].m - ch.pm) * a.c) / ch.ps;
+  double v[M], cum[M], total = 0.0;
+  for (;;) {
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      const int c = i * 256 + tid;
+      v[i] = 0.0;
+      if (c < a.nchunk)
+        v[i] = residual || !ch.residual ? mb[c] : rescaled(pb[c].s, pb[c].m, ch.pm, a.c) / ch.ps;
+      cum[i] = v[i];
+    }
+    total = block_scan(cum, s_w);
+    if (total > 0.0 || !residual) break;
+    residual = false;  // nothing left over: drawn from p
   }
-  const bool again = ch.residual != 0 && !residual;
-  auto chunk_mass = [&](int c) {
-    if (!again) return mb[c];
-    return pb[c].m == -INFINITY ? 0.0 : pb[c].s * pow2((pb[c].m - ch.pm) * a.c) / ch.ps;
-  };
   const double target = (double)a.u_sample[b] * total;
-  // the first chunk whose running sum passes the target; failing that (u of 1, rounding) the last with mass
-  int pick = -1, last = 0;
-  double before = 0.0, run = 0.0, before_last = 0.0;
-  for (int c = 0; c < a.nchunk; ++c) {
-    const double v = chunk_mass(c);
-    if (v > 0.0) {
-      last = c;
-      before_last = run;
-    }
-    if (pick < 0 && run + v > target) {
-      pick = c;
-      before = run;
-    }
-    run += v;
-  }
-  if (pick < 0) {
-    pick = last;
-    before = before_last;
-  }
   if (tid == 0) {
+    s_pick = INT_MAX;
+    s_any = 0;
     s_first = INT_MAX;
     s_last = -1;
   }
   __syncthreads();
+  // the first chunk whose running sum passes the target; failing that (u of 1, rounding) the last with mass
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+    if (v[i] > 0.0) {
+      atomicMax(&s_any, i * 256 + tid);
+      if (cum[i] > target) atomicMin(&s_pick, i * 256 + tid);
+    }
+  __syncthreads();
+  const int pick = s_pick < INT_MAX ? s_pick : s_any;
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+    if (i * 256 + tid == pick) s_before = cum[i] - v[i];
   const T* zp = (const T*)a.logits + (r0 + ch.acc) * a.ld_logits;
   const T* zq = residual && a.draft_logits ? (const T*)a.draft_logits + (d0 + ch.acc) * a.ld_draft : nullptr;
   const int y = residual && !a.draft_logits ? a.draft[d0 + ch.acc] : -1;
-  double at_start = before;
+  const double bp = -ch.pm * a.c, bq = -ch.qm * a.c, np = 1.0 / ch.ps, nq = 1.0 / ch.qs;
+  float x[I][E], xq[I][E];
+  double t[I][E], sum[I];
+#pragma unroll
   for (int i = 0; i < I; ++i) {
-    const int at = pick * kChunk + (i * 256 + tid) * E;
-    float x[E], xq[E];
-    double v[E];
-    load_logits(zp, at, a.V, x);
-    if (zq) load_logits(zq, at, a.V, xq);
-    double sum = 0.0;
+    load_logits(zp, pick * kChunk + (i * 256 + tid) * E, a.V, x[i]);
+    if (zq) load_logits(zq, pick * kChunk + (i * 256 + tid) * E, a.V, xq[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < I; ++i) {
+    sum[i] = 0.0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      v[e] = weight(x[e], ch.pm, a.c) / ch.ps;
-      if (zq) v[e] = fmax(v[e] - weight(xq[e], ch.qm, a.c) / ch.qs, 0.0);
-      if (at + e == y) v[e] = 0.0;
-      sum += v[e];
+      t[i][e] = mass_of(x[i][e], a.c, bp) * np;
+      if (zq) t[i][e] = fmax(t[i][e] - mass_of(xq[i][e], a.c, bq) * nq, 0.0);
+      if (pick * kChunk + (i * 256 + tid) * E + e == y) t[i][e] = 0.0;
+      sum[i] += t[i][e];
     }
-    double whole;
-    const double incl = block_scan(sum, s_w, &whole);
-    double cum = at_start + (incl - sum);
+  }
+  double upto[I];
+#pragma unroll
+  for (int i = 0; i < I; ++i) upto[i] = sum[i];
+  block_scan(upto, s_w);  // its barriers also order s_before
+  const double before = s_before;
+  int first = INT_MAX, last = -1;
+#pragma unroll
+  for (int i = 0; i < I; ++i) {
+    double run = before + (upto[i] - sum[i]);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      cum += v[e];
-      if (v[e] > 0.0) {
-        atomicMax(&s_last, at + e);
-        if (cum > target) atomicMin(&s_first, at + e);
+      run += t[i][e];
+      const int at = pick * kChunk + (i * 256 + tid) * E + e;
+      if (t[i][e] > 0.0) {
+        last = at;
+        if (run > target) first = min(first, at);
       }
     }
-    at_start += whole;
-    __syncthreads();
   }
+  if (first < INT_MAX) atomicMin(&s_first, first);
+  if (last >= 0) atomicMax(&s_last, last);
+  __syncthreads();
   if (tid == 0) {
     const int tok = s_first < INT_MAX ? s_first : s_last;
     const int64_t r = r0 + ch.acc;
@@ -402,14 +438,17 @@ hipError_t launch_draft_verify(int dtype, const VerifyArgs& a, void* part, doubl
   Choice* ch = static_cast<Choice*>(choice);
   const int64_t rows = a.n_draft + a.B + (a.draft_logits ? a.n_draft : 0);
   const unsigned grid = (unsigned)(rows * a.nchunk);
-  const dim3 grid2((unsigned)a.nchunk, (unsigned)a.B);
+  // Every workgroup of decide judges its sequence's drafts for itself, then takes `per` chunks: all of them apart while
+  // that fills the GPU, more to a workgroup for a larger batch.
+  const int per = (int)std::min<int64_t>(std::max<int64_t>((int64_t)a.nchunk * a.B / 2048, 1), a.nchunk);
+  const dim3 grid2((unsigned)((a.nchunk + per - 1) / per), (unsigned)a.B);
   if (dtype == RLK_DTYPE_BF16) {
     k_verify_stats<bf16_t><<<grid, 256, 0, s>>>(a, pt, status);
-    k_verify_decide<bf16_t><<<grid2, 256, 0, s>>>(a, pt, mass, ch, status);
+    k_verify_decide<bf16_t><<<grid2, 256, 0, s>>>(a, pt, mass, ch, per, status);
     k_verify_draw<bf16_t><<<(unsigned)a.B, 256, 0, s>>>(a, pt, mass, ch);
   } else {
     k_verify_stats<float><<<grid, 256, 0, s>>>(a, pt, status);
-    k_verify_decide<float><<<grid2, 256, 0, s>>>(a, pt, mass, ch, status);
+    k_verify_decide<float><<<grid2, 256, 0, s>>>(a, pt, mass, ch, per, status);
     k_verify_draw<float><<<(unsigned)a.B, 256, 0, s>>>(a, pt, mass, ch);
   }
   prof_mark(KK_VERIFY, false, s);
