@@ -754,18 +754,40 @@ __global__ void __launch_bounds__(256) k_kv_merge(KvArgs a, AttnArgs p, AttnPlan
   const int g = a.Hq / a.Hkv, row = blockIdx.y * RPB + tid / LPR, e = (tid % LPR) * 4;
   const int tok = d.rt * pl.tpt + row / g;
   if (row >= BM || row / g >= pl.tpt || tok >= s.n) return;
+  // The row's LPR lanes take a part each for its maximum and sum, then all of them the parts one by one.
+  const int jl = tid % LPR, parts = d.last - w + 1;
+  auto index = [&](int k) { return (int64_t)(k == 0 ? 2 * w + 1 : 2 * (w + k)) * BM + row; };
   float M = -INFINITY;
-  for (int k = w; k <= d.last; ++k) M = fmaxf(M, pl.ml[(int64_t)(k == w ? 2 * k + 1 : 2 * k) * BM + row].x);
+  for (int k = jl; k < parts; k += LPR) M = fmaxf(M, pl.ml[index(k)].x);
+#pragma unroll
+  for (int o = LPR / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  const float base = M == -INFINITY ? 0.0f : M;
   float L = 0.0f;
   f32x4 o = {0, 0, 0, 0};
-  for (int k = w; k <= d.last; ++k) {
-    const int64_t at = (int64_t)(k == w ? 2 * k + 1 : 2 * k) * BM + row;
-    const float2 ml = pl.ml[at];
-    if (ml.x == -INFINITY && ml.y == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml.x - M);
-    L += ml.y * f;
-    if (e < a.D) o += *reinterpret_cast<const f32x4*>(pl.part + at * DP + e) * f;
+  for (int k0 = 0; k0 < parts; k0 += LPR) {
+    float f = 0.0f;
+    if (k0 + jl < parts) {
+      const float2 ml = pl.ml[index(k0 + jl)];
+      f = __builtin_amdgcn_exp2f(ml.x - base);
+      L += ml.y * f;
+    }
+    const int n = min(LPR, parts - k0);
+    for (int k = 0; k < n; k += 8) {  // eight loads in flight
+      f32x4 v[8];
+      float fk[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int at = min(k + u, n - 1);
+        fk[u] = __shfl(f, (tid & 63) / LPR * LPR + at, 64);
+        v[u] = *reinterpret_cast<const f32x4*>(pl.part + index(k0 + at) * DP + e);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (k + u < n) o += v[u] * fk[u];
+    }
   }
+#pragma unroll
+  for (int q = LPR / 2; q > 0; q >>= 1) L += __shfl_xor(L, q, 64);
   const int64_t t = s.row0 + tok, qh = d.h * g + row % g;
   const float inv = L > 0.0f ? 1.0f / L : (L == 0.0f ? 0.0f : L);
   if (e < a.D) {
