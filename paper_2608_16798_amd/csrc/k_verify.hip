@@ -62,35 +62,59 @@ __device__ __forceinline__ float load_logit(const T* row, int i) {
   else return row[i];
 }
 
-// 2^t for t <= 0, to 2e-14 of its value; 2^-1000 below that.  The nearest whole number n comes out of the sum with
-// 1.5 2^52 (its low word), 2^f for the rest f in [-1/2, 1/2] out of the polynomial through the ten Chebyshev nodes of that
-// interval, and n goes into the exponent: fifteen fp64 operations, of which the whole pass is made.
-__device__ __forceinline__ double pow2(double t) {
-  t = fmax(t, -1000.0);
+// The bits of 2^(j / 32), less j 2^47: adding n 2^47 for n = 32 k + j leaves those of 2^(n / 32).
+__device__ const uint64_t kPow2Table[32] = {
+    0x3ff0000000000000ull, 0x3fefd9b0d3158574ull, 0x3fefb5586cf9890full, 0x3fef9301d0125b51ull,
+    0x3fef72b83c7d517bull, 0x3fef54873168b9aaull, 0x3fef387a6e756238ull, 0x3fef1e9df51fdee1ull,
+    0x3fef06fe0a31b715ull, 0x3feef1a7373aa9cbull, 0x3feedea64c123422ull, 0x3feece086061892dull,
+    0x3feebfdad5362a27ull, 0x3feeb42b569d4f82ull, 0x3feeab07dd485429ull, 0x3feea47eb03a5585ull,
+    0x3feea09e667f3bcdull, 0x3fee9f75e8ec5f74ull, 0x3feea11473eb0187ull, 0x3feea589994cce13ull,
+    0x3feeace5422aa0dbull, 0x3feeb737b0cdc5e5ull, 0x3feec49182a3f090ull, 0x3feed503b23e255dull,
+    0x3feee89f995ad3adull, 0x3feeff76f2fb5e47ull, 0x3fef199bdd85529cull, 0x3fef3720dcef9069ull,
+    0x3fef5818dcfba487ull, 0x3fef7c97337b9b5full, 0x3fefa4afa2a490daull, 0x3fefd0765b6e4540ull};
+
+// 2^(t / 32) for t <= 0, to 8e-14 of its value; 2^-1000 below that.  The nearest whole number n comes out of the sum with
+// 1.5 2^52 (its low word); 2^(f / 32) for the rest f in [-1/2, 1/2] out of the polynomial through the five Chebyshev
+// nodes of that interval, 2^((n mod 32) / 32) out of a table in LDS (an entry to each pair of its 64 banks: no
+// conflicts), and n / 32 goes into the exponent.  Eleven fp64 operations with the argument's, where nine powers without a
+// table take sixteen (the first pass over 1,152 rows of 151,936: 143 us and 152 us).
+__device__ __forceinline__ double pow2(double t, const double* tab) {
+  t = fmax(t, -32000.0);
   const double u = t + 6755399441055744.0, f = t - (u - 6755399441055744.0);
-  double p = 1.0205905413765595e-07;
-  p = fma(p, f, 1.325964524488711e-06);
-  p = fma(p, f, 1.5252672924850737e-05);
-  p = fma(p, f, 0.0001540343375125101);
-  p = fma(p, f, 0.0013333558200794592);
-  p = fma(p, f, 0.009618129193934313);
-  p = fma(p, f, 0.05550410866465167);
-  p = fma(p, f, 0.2402265069564034);
-  p = fma(p, f, 0.6931471805599462);
-  p = fma(p, f, 1.0000000000000135);
-  return __hiloint2double(__double2hiint(p) + (int)((uint32_t)__double2loint(u) << 20), __double2loint(p));
+  double p = 9.172607532092245e-09;
+  p = fma(p, f, 1.6938633903155644e-06);
+  p = fma(p, f, 0.0002345961981994449);
+  p = fma(p, f, 0.02166084939172217);
+  p = fma(p, f, 1.0);
+  const int n = __double2loint(u);
+  const double e = tab[n & 31];
+  return p * __hiloint2double(__double2hiint(e) + (int)((uint32_t)n << 15), __double2loint(e));
+}
+__device__ __forceinline__ void load_table(double* tab) {
+  if (threadIdx.x < 32) tab[threadIdx.x] = __longlong_as_double((long long)kPow2Table[threadIdx.x]);
 }
 
-// exp((z - m) / tau) with c = log2(e) / tau and b = -m c, the largest logit m finite
-__device__ __forceinline__ double weight(float z, double c, double b) { return pow2(fma((double)z, c, b)); }
+// exp((z - m) / tau) with c = 32 log2(e) / tau and b = -m c, the largest logit m finite
+__device__ __forceinline__ double weight(float z, double c, double b, const double* tab) {
+  return pow2(fma((double)z, c, b), tab);
+}
 // the same, exactly 0 where there is no mass
-__device__ __forceinline__ double mass_of(float z, double c, double b) {
+__device__ __forceinline__ double mass_of(float z, double c, double b, const double* tab) {
   const double t = fma((double)z, c, b);
-  return t < -999.0 ? 0.0 : pow2(t);
+  return t < -31968.0 ? 0.0 : pow2(t, tab);
 }
 // a chunk's sum against the row's largest logit
-__device__ __forceinline__ double rescaled(double s, double m, double row_m, double c) {
-  return m == -INFINITY ? s : s * pow2((m - row_m) * c);
+__device__ __forceinline__ double rescaled(double s, double m, double row_m, double c, const double* tab) {
+  return m == -INFINITY ? s : s * pow2((m - row_m) * c, tab);
+}
+
+// Maximum of three, of a number and a NaN the number.  (fmaxf quiets every operand first: one instruction more for each
+// logit, and the first pass is bound by the vector ALU, which it keeps 86 % busy.  With this and NaN looked for in pairs
+// 143 -> 128 us for 1,152 rows.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
 }
 
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -109,20 +133,21 @@ __global__ void __launch_bounds__(256) k_verify_stats(VerifyArgs a, Part* part, 
   const T* z = row < rows ? (const T*)a.logits + row * a.ld_logits : (const T*)a.draft_logits + (row - rows) * a.ld_draft;
   float x[I][E];
   float m = -INFINITY;
-  uint32_t top = 0;  // largest magnitude by its bits: above those of infinity, a NaN
+  bool nan = false;
 #pragma unroll
   for (int i = 0; i < I; ++i) load_logits(z, c * kChunk + (i * 256 + (int)threadIdx.x) * E, a.V, x[i]);
 #pragma unroll
   for (int i = 0; i < I; ++i)
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      m = fmaxf(m, x[i][e]);
-      top = max(top, __float_as_uint(x[i][e]) & 0x7fffffffu);
+    for (int e = 0; e < E; e += 2) {
+      m = max3(m, x[i][e], x[i][e + 1]);
+      nan |= __builtin_isunordered(x[i][e], x[i][e + 1]);
     }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
   __shared__ float s_m[4];
-  __shared__ double s_s[4];
+  __shared__ double s_s[4], s_tab[32];
+  load_table(s_tab);
   const int w = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) s_m[w] = m;
   __syncthreads();
@@ -133,9 +158,9 @@ __global__ void __launch_bounds__(256) k_verify_stats(VerifyArgs a, Part* part, 
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-      for (int e = 0; e < E; ++e) s += weight(x[i][e], a.c, b);
+      for (int e = 0; e < E; ++e) s += weight(x[i][e], a.c, b, s_tab);
   }
-  if (top > 0x7f800000u || m == INFINITY) s = NAN;
+  if (nan || m == INFINITY) s = NAN;
   s = wave_sum64(s);
   if ((threadIdx.x & 63) == 0) s_s[w] = s;
   __syncthreads();
@@ -143,7 +168,7 @@ __global__ void __launch_bounds__(256) k_verify_stats(VerifyArgs a, Part* part, 
 }
 
 // Largest logit and sum of a row from its chunks, by one wavefront.
-__device__ __forceinline__ Part row_total(const Part* part, int nchunk, double c) {
+__device__ __forceinline__ Part row_total(const Part* part, int nchunk, double c, const double* tab) {
   const int lane = threadIdx.x & 63;
   double m = -INFINITY;
   for (int i = lane; i < nchunk; i += 64) m = fmax(m, part[i].m);
@@ -152,7 +177,7 @@ __device__ __forceinline__ Part row_total(const Part* part, int nchunk, double c
   double s = 0.0;
   for (int i = lane; i < nchunk; i += 64) {
     const Part p = part[i];
-    s += rescaled(p.s, p.m, m, c);
+    s += rescaled(p.s, p.m, m, c, tab);
   }
   return {wave_sum64(s), m};
 }
@@ -180,7 +205,8 @@ __global__ void __launch_bounds__(256) k_verify_decide(VerifyArgs a, const Part*
   const int c = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, w = tid >> 6;
   __shared__ Part s_p[4], s_q[4];
   __shared__ int s_ok[4], s_bad[4];
-  __shared__ double s_sum[4];
+  __shared__ double s_sum[4], s_tab[32];
+  load_table(s_tab);
   const Span sp = span(a, b);
   if (b == 0 && c == 0 && tid == 0 && a.cu[0] != 0) atomicOr(status, RLK_DERR_CU_SEQLENS);
   if (sp.n < 0) {
@@ -191,12 +217,13 @@ __global__ void __launch_bounds__(256) k_verify_decide(VerifyArgs a, const Part*
     return;
   }
   const int64_t r0 = sp.d0 + b, rows = a.n_draft + a.B;
+  __syncthreads();
   // four drafts at a time, a wavefront each, up to the first that is not accepted; the last row has no draft
   int acc = 0, bad = 0, from = 0;
   for (int i0 = 0;; i0 += 4) {
     const int i = i0 + w;
     if (i <= sp.n) {
-      const Part p = row_total(part + (r0 + i) * a.nchunk, a.nchunk, a.c);
+      const Part p = row_total(part + (r0 + i) * a.nchunk, a.nchunk, a.c, s_tab);
       Part q = {1.0, 0.0};
       int ok = 0, wrong = p.s > 0.0 && p.m < INFINITY ? 0 : RLK_DERR_LOGITS;
       if (i < sp.n) {
@@ -206,11 +233,11 @@ __global__ void __launch_bounds__(256) k_verify_decide(VerifyArgs a, const Part*
         } else {
           double qy = 1.0;
           if (a.draft_logits) {
-            q = row_total(part + (rows + sp.d0 + i) * a.nchunk, a.nchunk, a.c);
+            q = row_total(part + (rows + sp.d0 + i) * a.nchunk, a.nchunk, a.c, s_tab);
             if (!(q.s > 0.0 && q.m < INFINITY)) wrong |= RLK_DERR_LOGITS;
-            qy = mass_of(load_logit((const T*)a.draft_logits + (sp.d0 + i) * a.ld_draft, y), a.c, -q.m * a.c) / q.s;
+            qy = mass_of(load_logit((const T*)a.draft_logits + (sp.d0 + i) * a.ld_draft, y), a.c, -q.m * a.c, s_tab) / q.s;
           }
-          const double py = mass_of(load_logit((const T*)a.logits + (r0 + i) * a.ld_logits, y), a.c, -p.m * a.c) / p.s;
+          const double py = mass_of(load_logit((const T*)a.logits + (r0 + i) * a.ld_logits, y), a.c, -p.m * a.c, s_tab) / p.s;
           ok = (double)a.u_accept[sp.d0 + i] * qy < py;
         }
       }
@@ -267,7 +294,7 @@ __global__ void __launch_bounds__(256) k_verify_decide(VerifyArgs a, const Part*
   for (int ch = c * per; ch < min(a.nchunk, (c + 1) * per); ++ch) {
     if (!residual || (!zq && y / kChunk != ch)) {
       const Part mine = part[(r0 + acc) * a.nchunk + ch];
-      if (tid == 0) mass[(int64_t)b * a.nchunk + ch] = rescaled(mine.s, mine.m, p.m, a.c) * np;
+      if (tid == 0) mass[(int64_t)b * a.nchunk + ch] = rescaled(mine.s, mine.m, p.m, a.c, s_tab) * np;
       continue;
     }
     float x[I][E], xq[I][E];
@@ -281,8 +308,8 @@ __global__ void __launch_bounds__(256) k_verify_decide(VerifyArgs a, const Part*
     for (int i = 0; i < I; ++i)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const double v = mass_of(x[i][e], a.c, bp) * np;
-        if (zq) sum += fmax(v - mass_of(xq[i][e], a.c, bq) * nq, 0.0);
+        const double v = mass_of(x[i][e], a.c, bp, s_tab) * np;
+        if (zq) sum += fmax(v - mass_of(xq[i][e], a.c, bq, s_tab) * nq, 0.0);
         else sum += ch * kChunk + (i * 256 + tid) * E + e == y ? 0.0 : v;
       }
     sum = wave_sum64(sum);
@@ -332,7 +359,9 @@ __global__ void __launch_bounds__(256) k_verify_draw(VerifyArgs a, const Part* p
   if (ch.acc < 0) return;
   __shared__ double s_w[I > M ? I : M][4];
   __shared__ int s_first, s_last, s_pick, s_any;
-  __shared__ double s_before;
+  __shared__ double s_before, s_tab[32];
+  load_table(s_tab);
+  __syncthreads();
   const int64_t d0 = a.cu[b], r0 = d0 + b;
   const double* mb = mass + (int64_t)b * a.nchunk;
   const Part* pb = part + (r0 + ch.acc) * a.nchunk;
@@ -344,7 +373,7 @@ __global__ void __launch_bounds__(256) k_verify_draw(VerifyArgs a, const Part* p
       const int c = i * 256 + tid;
       v[i] = 0.0;
       if (c < a.nchunk)
-        v[i] = residual || !ch.residual ? mb[c] : rescaled(pb[c].s, pb[c].m, ch.pm, a.c) / ch.ps;
+        v[i] = residual || !ch.residual ? mb[c] : rescaled(pb[c].s, pb[c].m, ch.pm, a.c, s_tab) / ch.ps;
       cum[i] = v[i];
     }
     total = block_scan(cum, s_w);
@@ -387,8 +416,8 @@ __global__ void __launch_bounds__(256) k_verify_draw(VerifyArgs a, const Part* p
     sum[i] = 0.0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      t[i][e] = mass_of(x[i][e], a.c, bp) * np;
-      if (zq) t[i][e] = fmax(t[i][e] - mass_of(xq[i][e], a.c, bq) * nq, 0.0);
+      t[i][e] = mass_of(x[i][e], a.c, bp, s_tab) * np;
+      if (zq) t[i][e] = fmax(t[i][e] - mass_of(xq[i][e], a.c, bq, s_tab) * nq, 0.0);
       if (pick * kChunk + (i * 256 + tid) * E + e == y) t[i][e] = 0.0;
       sum[i] += t[i][e];
     }

@@ -1258,7 +1258,7 @@ rlk_status_t rlk_draft_verify(const rlk_verify_t* p, const void* logits, const v
   a.n_accepted = n_accepted;
   a.logp = logp;
   a.inv_tau = p->temperature == 0.0f ? 1.0 : 1.0 / (double)p->temperature;
-  a.c = 1.4426950408889634 * a.inv_tau;
+  a.c = 32.0 * 1.4426950408889634 * a.inv_tau;
   RLK_TRY(launch_draft_verify(p->dtype, a, w + L.part, reinterpret_cast<double*>(w + L.mass), w + L.choice,
                               reinterpret_cast<int32_t*>(w + L.hdr), s),
           "draft_verify");

@@ -319,7 +319,7 @@ struct VerifyArgs {
   const float *u_accept, *u_sample;
   int32_t *tokens, *n_accepted;
   float* logp;
-  double c, inv_tau;  // log2(e) / tau, 1 / tau
+  double c, inv_tau;  // 32 log2(e) / tau, 1 / tau
 };
 int verify_chunks(int V);
 size_t verify_part_bytes(int64_t rows, int nchunk);
