@@ -55,6 +55,19 @@ __device__ __forceinline__ void block_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// 16 bytes a lane from base + off (zeros without a read where off + 16 passes size) to the wavefront's 1 KiB of LDS at dst.
+__device__ __forceinline__ void copy16(char* base, int size, char* dst, uint32_t off) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(base, (short)0, size, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, LDSP(dst), 16, off, 0, 0, 0);
+}
+
+// Maximum of three (fmaxf would quiet every operand first).  Not for a product's result before C code has read it: the
+// wait that needs is not put in front of an asm statement.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 // Maximum / sum of a lane and the one 32 further.
 __device__ __forceinline__ float swap_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -142,19 +155,22 @@ __device__ __forceinline__ void read_v(const int (&u)[N], u32x4 (&f)[N]) {
   for (int i = 0; i < N; ++i) f[i] = u32x4{l[i].x, l[i].y, h[i].x, h[i].y};
 }
 
-// Infinities and NaN of a fragment of values are taken out of it: a zero probability times one of them is NaN, so a row
-// that does not see the key would get it too.  They come back as counts (up: +inf, down: -inf, NaN in both) against
-// the probabilities' signs.
-__device__ __forceinline__ void take_nonfinite(u32x4& v, u32x4& up, u32x4& down) {
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const uint32_t x = v[w];
-    const uint32_t odd = ((((x & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xffffu;   // exponent all ones
-    const uint32_t nan = ((((x & 0x007f007fu) + 0x007f007fu) >> 7) & 0x00010001u) * 0xffffu;    // and a mantissa
+// Values of a tile that holds infinities or NaN, where some row does not see every key (a zero probability times one of
+// them is NaN, which would reach that row).  They are taken out for the product itself; two products more bring them
+// back where a probability is above zero: the largest finite number in place of +inf and NaN, then its negative in
+// place of -inf and NaN, against that number for each such probability.  Their product overflows to the infinity, and
+// both infinities make NaN.
+template <typename T>
+__device__ __forceinline__ uint32_t part_of_value(uint32_t x, int pass) {
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t odd = ((((x & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u) * 0xffffu;  // exponent all ones
+    const uint32_t nan = ((((x & 0x007f007fu) + 0x007f007fu) >> 7) & 0x00010001u) * 0xffffu;   // a mantissa
     const uint32_t neg = ((x >> 15) & 0x00010001u) * 0xffffu;
-    up[w] = odd & (nan | ~neg) & 0x3f803f80u;
-    down[w] = odd & (nan | neg) & 0x3f803f80u;
-    v[w] = x & ~odd;
+    return pass == 0 ? x & ~odd : pass == 1 ? odd & (nan | ~neg) & 0x7f7f7f7fu : odd & (nan | neg) & 0xff7fff7fu;
+  } else {
+    const float v = __uint_as_float(x);
+    const bool odd = !(fabsf(v) < INFINITY);
+    return pass == 0 ? (odd ? 0u : x) : pass == 1 ? (odd && !(v < 0.0f) ? 0x7f7fffffu : 0u) : odd && !(v > 0.0f) ? 0xff7fffffu : 0u;
   }
 }
 
@@ -292,7 +308,27 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
   const int64_t row_bytes = (int64_t)a.D * ESZ;
   const int64_t head_bytes = row_bytes << a.ps_shift, page_bytes = a.Hkv * head_bytes;
   const bool paged_rows = (1 << a.ps_shift) >= G::RPI;  // the rows of a copy lie in one page
+  const int run = min(1 << a.ps_shift, C::LROWS);       // rows of a wavefront's share of a tile that lie in one page
   const int crow = lane / CPR, cchunk = lane % CPR;
+  // where a lane's 16 bytes of copy i lie, from the run's first row on: the chunk that its place in LDS holds
+  auto copy_offset = [&](int i, bool value) {
+    const int lr = wm * C::LROWS + i * G::RPI + crow;
+    const int ck = cchunk ^ (value ? G::v_swz(lr) : G::k_swz(lr));
+    const uint32_t row = ((i * G::RPI) & (run - 1)) + crow;
+    return ck * EPC < a.D ? row * (uint32_t)row_bytes + ck * 16 : 0x80000000u;
+  };
+  uint32_t offs[NI <= 8 ? NI : 1][2];
+  if constexpr (NI <= 8) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      offs[i][0] = copy_offset(i, false);
+      offs[i][1] = copy_offset(i, true);
+    }
+  }
+  auto copy_at = [&](int i, bool value) {
+    if constexpr (NI <= 8) return offs[i][value];
+    else return copy_offset(i, value);
+  };
   // key and value fragments
   const int k_base = kw * C::PART + ql * G::ROWB + ((hl ^ G::k_swz(ql)) << 4);
   int v_base[DB < 4 ? DB : 4];
@@ -375,36 +411,47 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
       __syncthreads();
 
       // ---- copies of this wavefront's rows of a tile into a stage
+      // (the page indices of a tile are read from LDS a tile before: one lane for each copy)
+      auto pages_of = [&](int t) {
+        const int key = t * C::TK + kw * C::PK + wm * C::LROWS + min(lane, NI - 1) * G::RPI;
+        return s_pages[min((key >> a.ps_shift) - pg0, kPageCap - 1)];
+      };
+      int pages = pages_of(t0);
       auto copy_tile = [&](int t, int stage) {
-        if (t >= t1) t = t1 - 1;  // keeps the count of copies in flight; nobody reads it
         const int part0 = t * C::TK + kw * C::PK + wm * C::LROWS;  // first key of the share
         char* dst = smem + stage * C::STAGE + kw * C::PART + wm * C::LROWS * G::ROWB;
         if (paged_rows) {
-          // page of each copy, one lane each
-          const int kk = part0 + (lane < NI ? lane : 0) * G::RPI;
-          const int pv = s_pages[min((kk >> a.ps_shift) - pg0, kPageCap - 1)];
-#pragma unroll NI <= 4 ? NI : 2
-          for (int i = 0; i < NI; ++i) {
+          // A run of rows in one page: rows behind its end in the sequence, and the whole of a tile behind the segment
+          // (which only keeps the count of copies in flight), lie past the buffer's size and are zeros without a read.
+          int64_t at = 0;
+          int size = 0;
+          auto begin_run = [&](int i) {
             const int key = part0 + i * G::RPI;
-            const int pg = __builtin_amdgcn_readlane(pv, i);
-            const int in = key & ((1 << a.ps_shift) - 1);
-            const int rows = min((1 << a.ps_shift) - in, s.len - key);  // rows from here on in the page and the sequence
-            const uint32_t size = pg >= 0 && rows > 0 ? (uint32_t)rows * (uint32_t)row_bytes : 0u;
-            const int64_t at = pg >= 0 ? pg * page_bytes + head0 + in * row_bytes : 0;
-            const int lr = wm * C::LROWS + i * G::RPI + crow;
-            const int ck = cchunk ^ G::k_swz(lr), cv = cchunk ^ G::v_swz(lr);
-            const uint32_t ro = crow * (uint32_t)row_bytes;
-            const uint32_t ok = ck * EPC < a.D ? ro + ck * 16 : 0x80000000u;
-            const uint32_t ov = cv * EPC < a.D ? ro + cv * 16 : 0x80000000u;
-            const __amdgpu_buffer_rsrc_t rk =
-                __builtin_amdgcn_make_buffer_rsrc((char*)a.k_pages + at, (short)0, (int)size, 0x00020000);
-            const __amdgpu_buffer_rsrc_t rv =
-                __builtin_amdgcn_make_buffer_rsrc((char*)a.v_pages + at, (short)0, (int)size, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, LDSP(dst + i * 1024), 16, ok, 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, LDSP(dst + C::WK * C::PART + i * 1024), 16, ov, 0, 0, 0);
+            const int pg = __builtin_amdgcn_readlane(pages, i);
+            const int rows = min(run, s.len - key);
+            const bool in_use = pg >= 0 && rows > 0 && t < t1;
+            at = in_use ? pg * page_bytes + head0 + (key & ((1 << a.ps_shift) - 1)) * row_bytes : 0;
+            size = in_use ? rows * (int)row_bytes : 0;
+          };
+          auto copy = [&](int i) {
+            copy16((char*)a.k_pages + at, size, dst + i * 1024, copy_at(i, false));
+            copy16((char*)a.v_pages + at, size, dst + C::WK * C::PART + i * 1024, copy_at(i, true));
+          };
+          if (run == C::LROWS) {
+            begin_run(0);
+#pragma unroll NI <= 8 ? NI : 4
+            for (int i = 0; i < NI; ++i) copy(i);
+          } else {
+#pragma unroll NI <= 8 ? NI : 4
+            for (int i = 0; i < NI; ++i) {
+              if (((i * G::RPI) & (run - 1)) == 0) begin_run(i);
+              copy(i);
+            }
           }
+          pages = pages_of(t + 1);
         } else {
-          // pages smaller than a copy's rows: every lane finds its own; rows behind the sequence repeat its last
+          // pages smaller than a copy's rows: every lane finds its own; rows behind the sequence repeat its last (and a
+          // tile behind the segment is whatever, never read)
           const int nch = a.D / EPC;
 #pragma unroll 1
           for (int i = 0; i < NI; ++i) {
@@ -448,11 +495,21 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
           if (p.slot_end) wait_vmcnt<(NS - 2) * (2 * NI + 1)>();
           else wait_vmcnt<(NS - 2) * 2 * NI>();
         }
-        // A part that some row does not see whole: masked, and its values are looked through for NaN and infinities,
-        // which a zero probability does not keep out of a product.
-        const bool masked = part0 + C::PK - 1 > (C::WM == 1 ? first_slot : ctx + tok0) || p.slot_end != nullptr;
+        // What the rows see of the part: nothing (passed over), all of it, or some (masked; and its values are looked
+        // through for NaN and infinities, which a zero probability does not keep out of a product).
+        bool all_after = true, some_after = true;  // keys whose subtree lasts past the wavefront's last / first slot
+        bool all_wg = true, some_wg = true;        // the same for the workgroup's rows
+        if (p.slot_end) {
+          const int e = s_ends[stage * C::TK + kw * C::PK + (lane < C::PK ? lane : 0)];
+          all_after = __all(e > last_slot);
+          some_after = __any(e > first_slot);
+          all_wg = __all(e > ctx + tok0 + ntok - 1);
+          some_wg = __any(e > ctx + tok0);
+        }
+        const bool active = part0 <= last_slot && some_after;
+        const bool odd_matters = !(part0 + C::PK - 1 <= ctx + tok0 && all_wg) && part0 <= ctx + tok0 + ntok - 1 && some_wg;
         const char* kst = smem + stage * C::STAGE;
-        if (masked) {
+        if (odd_matters) {
           uint32_t odd = 0;
           const char* v0 = kst + (C::WK + kw) * C::PART + wm * C::LROWS * G::ROWB + lane * 16;
 #pragma unroll
@@ -471,56 +528,84 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
           block_barrier();
           copy_tile(t + NS - 1, stage == 0 ? NS - 1 : stage - 1);
         }
-        if (part0 <= last_slot) {
-          // ---- scores
-          f32x16 sc[NB];
+        // this wavefront's share of the tile's values, as pass `pass` takes them
+        auto odd_values = [&](int pass) {
+          char* v0 = smem + stage * C::STAGE + (C::WK + kw) * C::PART + wm * C::LROWS * G::ROWB + lane * 16;
+#pragma unroll 1
+          for (int i = 0; i < NI; ++i) {
+            u32x4 v = *reinterpret_cast<const u32x4*>(v0 + i * 1024);
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
+            for (int w = 0; w < 4; ++w) v[w] = part_of_value<T>(v[w], pass);
+            *reinterpret_cast<u32x4*>(v0 + i * 1024) = v;
+          }
+          if constexpr (C::WM > 1) block_barrier();
+        };
+        bool poisoned = false;
+        if (odd_matters) {
+          int any = 0;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sc[nb][r] = 0.0f;
+          for (int w = 0; w < C::WM; ++w) any |= s_flag[stage * 8 + (C::WM > 1 ? w : wid)];
+          poisoned = __builtin_amdgcn_readfirstlane(any) != 0;
+          if (poisoned) odd_values(0);
+        }
+        f32x16 sc[NB];
+        if (active) {
+          // ---- scores: a group of key fragments ahead of the products
+          constexpr int KS = CPR / 2, GR = ESZ == 2 ? 4 : 2, NG = NB * KS / GR;
+          u32x4 kf[2][GR];
+          auto read_k = [&](int i) {
 #pragma unroll
-            for (int ks = 0; ks < CPR / 2; ++ks) {
-              const u32x4 kf = *reinterpret_cast<const u32x4*>(kst + ((k_base + nb * 32 * G::ROWB) ^ (ks << 5)));
+            for (int j = 0; j < GR; ++j) {
+              const int nb = j % NB, ks = (i * GR + j) / NB;  // neighbouring products are independent
+              kf[i & 1][j] = *reinterpret_cast<const u32x4*>(kst + ((k_base ^ (ks << 5)) + nb * 32 * G::ROWB));
+            }
+          };
+          read_k(0);
+#pragma unroll
+          for (int i = 0; i < NG; ++i) {
+            if (i + 1 < NG) read_k(i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < GR; ++j) {
+              const int nb = j % NB, ks = (i * GR + j) / NB;
+              if (ks == 0) sc[nb] = f32x16{};
+              const u32x4 kv = kf[i & 1][j];
               if constexpr (ESZ == 2) {
-                sc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf),
+                sc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kv),
                                                                  __builtin_bit_cast(bf16x8, qf[ks]), sc[nb], 0, 0, 0);
               } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  sc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qf[ks][e]), sc[nb], 0,
+                  sc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kv[e]), __uint_as_float(qf[ks][e]), sc[nb], 0,
                                                                 0, 0);
               }
             }
+            __builtin_amdgcn_sched_barrier(0);
           }
-          bool poisoned = false;
-          if (masked) {
-            int any = 0;
-#pragma unroll
-            for (int w = 0; w < C::WM; ++w) any |= s_flag[stage * 8 + (C::WM > 1 ? w : wid)];
-            poisoned = __builtin_amdgcn_readfirstlane(any) != 0;
+          if (part0 + C::PK - 1 > first_slot) {
             const int rel = qslot - part0 - 4 * hl;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
               for (int r = 0; r < 16; ++r) sc[nb][r] = nb * 32 + key_of(r, 0) > rel ? -INFINITY : sc[nb][r];
-            if (p.slot_end) {
-              const int* ends = s_ends + stage * C::TK + kw * C::PK + 4 * hl;
+          }
+          if (!all_after) {
+            const int* ends = s_ends + stage * C::TK + kw * C::PK + 4 * hl;
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb)
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                  const u32x4 e = *reinterpret_cast<const u32x4*>(ends + nb * 32 + 2 * r);
+              for (int r = 0; r < 16; r += 4) {
+                const u32x4 e = *reinterpret_cast<const u32x4*>(ends + nb * 32 + 2 * r);
 #pragma unroll
-                  for (int i = 0; i < 4; ++i) sc[nb][r + i] = (int)e[i] <= qslot ? -INFINITY : sc[nb][r + i];
-                }
-            }
+                for (int i = 0; i < 4; ++i) sc[nb][r + i] = (int)e[i] <= qslot ? -INFINITY : sc[nb][r + i];
+              }
           }
           // ---- running maximum and sum
-          float mx = sc[0][0];
+          float mx = fmaxf(sc[0][0], sc[NB - 1][15]);  // in C: the compiler waits for the last product here
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[nb][r]);
+            for (int r = 0; r < 16; r += 2) mx = max3(mx, sc[nb][r], sc[nb][r + 1]);
           mx = swap_max(mx);
           if (__any((mx - m) * c > kLazy || (m == -INFINITY && mx > m))) {
             const float m2 = fmaxf(m, mx);
@@ -542,84 +627,69 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
               sum += sc[nb][r];
             }
           l += sum;
-          // ---- values
-          if constexpr (ESZ == 2) {
-            int u[VB];
+        }
+        // ---- values
+        for (int pass = 0;;) {
+          if (active) {
+            if constexpr (ESZ == 2) {
+              int u[VB];
 #pragma unroll
-            for (int d = 0; d < VB; ++d) u[d] = v_base[d] + stage * C::STAGE;
-            auto step = [&](auto NBK, auto SK) {
-              constexpr int nb = decltype(NBK)::value, sk = decltype(SK)::value;
-              u32x4 pf;
+              for (int d = 0; d < VB; ++d) u[d] = v_base[d] + stage * C::STAGE;
+              // 16 keys and up to four 32-wide blocks of the head
+              auto step = [&](auto K, auto D0) {
+                constexpr int k = decltype(K)::value, d0 = decltype(D0)::value;
+                u32x4 vf[VB], pf;
+                read_v<VB, k * 16 * G::ROWB + d0 * 64, 8 * G::ROWB>(u, vf);
 #pragma unroll
-              for (int w = 0; w < 4; ++w) pf[w] = pack_bf16x2(sc[nb][sk * 8 + 2 * w], sc[nb][sk * 8 + 2 * w + 1]);
-              constexpr int off = (nb * 32 + sk * 16) * G::ROWB;
-              auto blocks = [&](auto D0) {
-                constexpr int d0 = decltype(D0)::value;
-                u32x4 vf[VB];
-                read_v<VB, off + d0 * 64, 8 * G::ROWB>(u, vf);
-                if (poisoned) {
-                  u32x4 ind;
-#pragma unroll
-                  for (int w = 0; w < 4; ++w)
-                    ind[w] = (sc[nb][sk * 8 + 2 * w] > 0.0f ? 0x3f80u : 0u) | (sc[nb][sk * 8 + 2 * w + 1] > 0.0f ? 0x3f800000u : 0u);
-#pragma unroll
-                  for (int d = 0; d < VB; ++d) {
-                    u32x4 up, down;
-                    take_nonfinite(vf[d], up, down);
-                    f32x16 t = {};
-                    t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, up), __builtin_bit_cast(bf16x8, ind),
-                                                                t, 0, 0, 0);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[d0 + d][r] += t[r] > 0.0f ? INFINITY : 0.0f;
-                    t = f32x16{};
-                    t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, down),
-                                                                __builtin_bit_cast(bf16x8, ind), t, 0, 0, 0);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[d0 + d][r] -= t[r] > 0.0f ? INFINITY : 0.0f;
-                  }
-                }
+                for (int w = 0; w < 4; ++w)
+                  pf[w] = pack_bf16x2(sc[k / 2][(k & 1) * 8 + 2 * w], sc[k / 2][(k & 1) * 8 + 2 * w + 1]);
 #pragma unroll
                 for (int d = 0; d < VB; ++d)
                   acc[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]),
                                                                         __builtin_bit_cast(bf16x8, pf), acc[d0 + d], 0, 0, 0);
               };
-              blocks(std::integral_constant<int, 0>{});
-              if constexpr (DB > 4) blocks(std::integral_constant<int, 4>{});
-            };
-            step(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
-            step(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
-            if constexpr (NB > 1) {
-              step(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{});
-              step(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
+              auto steps = [&](auto K) {
+                step(K, std::integral_constant<int, 0>{});
+                if constexpr (DB > 4) step(K, std::integral_constant<int, 4>{});
+              };
+              steps(std::integral_constant<int, 0>{});
+              steps(std::integral_constant<int, 1>{});
+              if constexpr (NB > 1) {
+                steps(std::integral_constant<int, 2>{});
+                steps(std::integral_constant<int, 3>{});
+              }
+            } else {
+              const char* v0 = kst + (C::WK + kw) * C::PART;
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                  const int k = nb * 32 + key_of(r, 0);  // half 1: 4 rows on
+                  const int rowb = (k + 4 * hl) * G::ROWB;
+#pragma unroll
+                  for (int d = 0; d < DB; ++d) {
+                    const int chunk = (d * 8 + (ql >> 2)) ^ (((k + 4 * hl) & 4) << 1);
+                    const float v = *reinterpret_cast<const float*>(v0 + rowb + chunk * 16 + (ql & 3) * 4);
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[nb][r], acc[d], 0, 0, 0);
+                  }
+                }
             }
-          } else {
-            const char* v0 = kst + (C::WK + kw) * C::PART;
+          }
+          if (__builtin_expect(!poisoned, 1) || ++pass == 3) break;
+          // the tile once more, for the next part of its values
+          if constexpr (C::WM > 1) block_barrier();
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          pages = pages_of(t);
+          copy_tile(t, stage);
+          pages = pages_of(t + NS);
+          wait_vmcnt<0>();
+          odd_values(pass);
+          if (pass == 1 && active) {
+            const float most = ESZ == 2 ? 3.3895314e38f : 3.4028235e38f;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const int k = nb * 32 + key_of(r, 0);  // half 1: 4 rows on
-                const int rowb = (k + 4 * hl) * G::ROWB;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                  const int chunk = (d * 8 + (ql >> 2)) ^ (((k + 4 * hl) & 4) << 1);
-                  float v = *reinterpret_cast<const float*>(v0 + rowb + chunk * 16 + (ql & 3) * 4);
-                  if (poisoned) {
-                    const float ind = sc[nb][r] > 0.0f ? 1.0f : 0.0f;
-                    const bool odd = !(fabsf(v) < INFINITY);
-                    f32x16 t = {};
-                    t = __builtin_amdgcn_mfma_f32_32x32x2f32(odd && !(v < 0.0f) ? 1.0f : 0.0f, ind, t, 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[d][i] += t[i] > 0.0f ? INFINITY : 0.0f;
-                    t = f32x16{};
-                    t = __builtin_amdgcn_mfma_f32_32x32x2f32(odd && !(v > 0.0f) ? 1.0f : 0.0f, ind, t, 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[d][i] -= t[i] > 0.0f ? INFINITY : 0.0f;
-                    v = odd ? 0.0f : v;
-                  }
-                  acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, sc[nb][r], acc[d], 0, 0, 0);
-                }
-              }
+              for (int r = 0; r < 16; ++r) sc[nb][r] = sc[nb][r] > 0.0f ? most : 0.0f;
           }
         }
         stage = stage + 1 == NS ? 0 : stage + 1;
