@@ -160,18 +160,23 @@ def _tensor(t, name: str, shape=None, dtypes=None, optional: bool = False, min_b
     `dtypes`, of exactly `shape` (None entries match any size) and contiguous (row-major).
     Raises TypeError / ValueError; nothing is launched.  Devices are checked afterwards, for all
     arguments together, by _on_one_gpu."""
-    import torch
-
     if t is None:
         if optional:
             return
         raise ValueError(f"{name} is required")
+    import torch
+
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
     if dtypes is not None and t.dtype not in dtypes:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
     if shape is not None:
-        ok = t.dim() == len(shape) and all(w is None or int(a) == int(w) for a, w in zip(t.shape, shape))
+        have = t.shape
+        ok = len(have) == len(shape)
+        if ok:
+            for a, w in zip(have, shape):
+                if w is not None and a != w:
+                    ok = False
         if not ok:
             want = "[" + ", ".join("*" if w is None else str(int(w)) for w in shape) + "]"
             raise ValueError(f"{name} has shape {list(t.shape)}, expected {want}")
@@ -187,12 +192,13 @@ def _on_one_gpu(**tensors):
     for name, t in tensors.items():
         if t is None:
             continue
-        if not t.is_cuda:
+        at = t.get_device()  # -1: not on a GPU
+        if at < 0:
             raise ValueError(f"{name} must be a GPU tensor, got device {t.device}")
         if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, other arguments on {dev}")
+            dev = at
+        elif at != dev:
+            raise ValueError(f"{name} is on {t.device}, other arguments on cuda:{dev}")
 
 
 def _float_types():
@@ -729,14 +735,17 @@ def _token_rows(t, name: str, heads, dim, dtype, tokens=None):
         raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    want = (tokens, heads, dim)
-    if t.dim() != 3 or any(w is not None and int(a) != int(w) for a, w in zip(t.shape, want)):
-        raise ValueError(f"{name} has shape {list(t.shape)}, expected "
+    have = t.shape
+    if (len(have) != 3 or have[2] != dim or (heads is not None and have[1] != heads)
+            or (tokens is not None and have[0] != tokens)):
+        want = (tokens, heads, dim)
+        raise ValueError(f"{name} has shape {list(have)}, expected "
                          f"[{', '.join('*' if w is None else str(int(w)) for w in want)}]")
-    n, h, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
-        raise ValueError(f"{name} must hold the heads of a token together (strides {list(t.stride())})")
-    return t.stride(0) if n > 1 else h * d
+    n, h, d = have
+    s0, s1, s2 = t.stride()
+    if (d > 1 and s2 != 1) or (h > 1 and s1 != d):
+        raise ValueError(f"{name} must hold the heads of a token together (strides {[s0, s1, s2]})")
+    return s0 if n > 1 else h * d
 
 
 def _check_cache(k_pages, v_pages, page_table, kv_len, cu_new):
@@ -756,10 +765,10 @@ def _check_cache(k_pages, v_pages, page_table, kv_len, cu_new):
 def make_cache(k_pages, v_pages, page_table, kv_len, cu_new, T, n_q_heads, max_new: int = 0) -> KvCache:
     """Cache descriptor (rlk_kv_t); max_new is an optional host-known bound on a sequence's new tokens."""
     n_pages, n_kv_heads, page_size, head_dim = k_pages.shape
-    return KvCache(T=T, B=kv_len.shape[0], n_pages=n_pages, page_size=page_size, max_pages=page_table.shape[1],
-                   n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=_dtype_code(k_pages),
-                   k_pages=_ptr(k_pages), v_pages=_ptr(v_pages), page_table=_ptr(page_table), kv_len=_ptr(kv_len),
-                   cu_new=_ptr(cu_new), max_new=int(max_new))
+    B, max_pages = page_table.shape
+    return KvCache(T, B, n_pages, page_size, max_pages, n_q_heads, n_kv_heads, head_dim, _dtype_code(k_pages),
+                   k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), kv_len.data_ptr(), cu_new.data_ptr(),
+                   int(max_new), 0)
 
 
 def kv_workspace_size(cache: KvCache) -> int:
@@ -768,11 +777,16 @@ def kv_workspace_size(cache: KvCache) -> int:
     return n.value
 
 
-def _gpu_scope(device):
-    """Makes `device` current for a launch (the current stream is that device's then)."""
+def _on_device(t, call, stream):
+    """call(stream handle) with t's GPU as the current one; without a stream, on that GPU's current stream.  (The
+    handle alone: a Stream object costs 3 us of a call of 20.)"""
     import torch
 
-    return torch.cuda.device(device)
+    at = t.get_device()
+    if at != torch.cuda.current_device():
+        with torch.cuda.device(at):
+            return call(torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+    return call(torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
 
 
 def kv_append(k_pages, v_pages, page_table, kv_len, cu_new, q, k, v, freq=None, positions=None, q_norm=None, k_norm=None,
@@ -813,9 +827,9 @@ def kv_append(k_pages, v_pages, page_table, kv_len, cu_new, q, k, v, freq=None, 
         q_out = torch.empty(T, Hq, D, dtype=dt, device=q.device)
     if ws is None:
         ws = alloc_workspace(kv_workspace_size(c), k_pages.device)
-    with _gpu_scope(k_pages.device):
-        _check(lib.rlk_kv_append(ctypes.byref(c), ctypes.byref(r), _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(positions),
-                                 _ptr(q_out), _ptr(ws), ws.numel(), _stream_handle(stream)))
+    _check(_on_device(k_pages, lambda s: lib.rlk_kv_append(
+        ctypes.byref(c), ctypes.byref(r), _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(positions), _ptr(q_out), _ptr(ws),
+        ws.numel(), s), stream))
     return q_out, ws
 
 
@@ -843,10 +857,9 @@ def kv_attention(q, k_pages, v_pages, page_table, kv_len, cu_new, scale=None, sl
         out = torch.empty(T, Hq, D, dtype=dt, device=q.device)
     if ws is None:
         ws = alloc_workspace(kv_workspace_size(c), q.device)
-    with _gpu_scope(q.device):
-        _check(lib.rlk_kv_attention(ctypes.byref(c), _ptr(q), qs, _ptr(slot_end),
-                                    0 if slot_end is None else slot_end.shape[1], D ** -0.5 if scale is None else scale,
-                                    _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream_handle(stream)))
+    _check(_on_device(q, lambda s: lib.rlk_kv_attention(
+        ctypes.byref(c), _ptr(q), qs, _ptr(slot_end), 0 if slot_end is None else slot_end.shape[1],
+        D ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), s), stream))
     return out, lse, ws
 
 
@@ -893,10 +906,9 @@ def draft_verify(logits, draft, cu_draft, u_accept, u_sample, draft_logits=None,
         logp = torch.empty(rows, dtype=torch.float32, device=dev)
     if ws is None:
         ws = alloc_workspace(verify_workspace_size(p), dev)
-    with _gpu_scope(dev):
-        _check(lib.rlk_draft_verify(ctypes.byref(p), _ptr(logits), _ptr(draft_logits), _ptr(draft), _ptr(cu_draft),
-                                    _ptr(u_accept), _ptr(u_sample), _ptr(tokens), _ptr(n_accepted), _ptr(logp), _ptr(ws),
-                                    ws.numel(), _stream_handle(stream)))
+    _check(_on_device(logits, lambda s: lib.rlk_draft_verify(
+        ctypes.byref(p), _ptr(logits), _ptr(draft_logits), _ptr(draft), _ptr(cu_draft), _ptr(u_accept), _ptr(u_sample),
+        _ptr(tokens), _ptr(n_accepted), _ptr(logp), _ptr(ws), ws.numel(), s), stream))
     return tokens, n_accepted, logp, ws
 
 

@@ -174,6 +174,19 @@ __device__ __forceinline__ uint32_t part_of_value(uint32_t x, int pass) {
   }
 }
 
+// The same by the compiler's own reads, which it may place and wait for one by one.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+template <int N, int OFF, int STEP>
+__device__ __forceinline__ void read_v_free(const int (&u)[N], u32x4 (&f)[N]) {
+  typedef __attribute__((address_space(3))) s16x4* P;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const u32x2 l = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(u[i] + OFF)));
+    const u32x2 h = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(u[i] + OFF + STEP)));
+    f[i] = u32x4{l.x, l.y, h.x, h.y};
+  }
+}
+
 // Key of register r of a 32 x 32 result in the lanes of half h.
 __device__ __forceinline__ constexpr int key_of(int r, int h) { return (r & 3) + 8 * (r >> 2) + 4 * h; }
 
@@ -639,7 +652,8 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
               auto step = [&](auto K, auto D0) {
                 constexpr int k = decltype(K)::value, d0 = decltype(D0)::value;
                 u32x4 vf[VB], pf;
-                read_v<VB, k * 16 * G::ROWB + d0 * 64, 8 * G::ROWB>(u, vf);
+                if constexpr (C::WM > 1) read_v_free<VB, k * 16 * G::ROWB + d0 * 64, 8 * G::ROWB>(u, vf);
+                else read_v<VB, k * 16 * G::ROWB + d0 * 64, 8 * G::ROWB>(u, vf);
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
                   pf[w] = pack_bf16x2(sc[k / 2][(k & 1) * 8 + 2 * w], sc[k / 2][(k & 1) * 8 + 2 * w + 1]);
