@@ -974,7 +974,7 @@ hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, in
   const Layout L = layout(sh.DP, sh.wgs, sh.BM);
   AttnPlan pl = {};
   pl.tpt = sh.tpt;
-  pl.min_piece = 512;
+  pl.min_piece = 128;
   pl.desc = reinterpret_cast<MergeDesc*>(ws + L.desc);
   pl.flags = reinterpret_cast<int32_t*>(ws + L.flags);
   pl.ml = reinterpret_cast<float2*>(ws + L.ml);
