@@ -15,6 +15,7 @@
 // k_kv_merge joins in order.  One token over a long history and a batch of ragged ones are the same to it.
 #include "rlk_internal.h"
 
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -27,6 +28,8 @@ namespace {
 
 constexpr float kLn2f = 0.6931471805599453f, kLog2ef = 1.4426950408889634f;
 constexpr int kPageCap = 1024;     // page indices held in LDS
+constexpr int kLiveCap = 512;      // tiles looked through at once, with subtree ends
+constexpr int kWhole = 1 << 30;    // mark of a tile that every row sees whole
 constexpr int kItemCost = 96;      // cost of starting a row tile, in keys
 constexpr float kLazy = 8.0f;      // the maximum may be passed by 2^8 before the sums are rescaled
 
@@ -61,13 +64,6 @@ __device__ __forceinline__ void copy16(char* base, int size, char* dst, uint32_t
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, LDSP(dst), 16, off, 0, 0, 0);
 }
 
-// Maximum of three (fmaxf would quiet every operand first).  Not for a product's result before C code has read it: the
-// wait that needs is not put in front of an asm statement.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
 // Maximum / sum of a lane and the one 32 further.
 __device__ __forceinline__ float swap_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -115,8 +111,8 @@ struct Cfg : Geo<T, DP_> {
   static constexpr int ENDS = NS * STAGE;                                          // int [NS][TK]: slot_end of the keys
   static constexpr int PAGES = ENDS + NS * TK * 4;                                 // int [kPageCap]
   static constexpr int FLAG = PAGES + kPageCap * 4;                                // int [NS][8]: non-finite values
-  static constexpr int MISC = FLAG + NS * 8 * 4;
-  static constexpr int LDS = MISC + 64;
+  static constexpr int LIVE = FLAG + NS * 8 * 4;                                   // int [kLiveCap]: tiles that some row sees
+  static constexpr int LDS = LIVE + (kLiveCap + 2) * 4;
   // joining the key groups: fp32 [WK][32][DP + 4] and m, l [WK][32], in the stages
   static constexpr int OROW = DP + 4;
   static_assert(WK == 1 || WK * 32 * OROW * 4 + WK * 32 * 8 <= NS * STAGE, "joining fits the stages");
@@ -174,19 +170,6 @@ __device__ __forceinline__ uint32_t part_of_value(uint32_t x, int pass) {
   }
 }
 
-// The same by the compiler's own reads, which it may place and wait for one by one.
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-template <int N, int OFF, int STEP>
-__device__ __forceinline__ void read_v_free(const int (&u)[N], u32x4 (&f)[N]) {
-  typedef __attribute__((address_space(3))) s16x4* P;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const u32x2 l = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(u[i] + OFF)));
-    const u32x2 h = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(u[i] + OFF + STEP)));
-    f[i] = u32x4{l.x, l.y, h.x, h.y};
-  }
-}
-
 // Key of register r of a 32 x 32 result in the lanes of half h.
 __device__ __forceinline__ constexpr int key_of(int r, int h) { return (r & 3) + 8 * (r >> 2) + 4 * h; }
 
@@ -231,15 +214,88 @@ struct AttnPlan {
   float2* ml;         // [2 workgroups][BM]: maximum (powers of 2) and sum of a part: 2 w the tail of a tile, 2 w + 1 its head
   float* part;        // [2 workgroups][BM][DP]
   int32_t* status;
+  // with subtree ends, from k_kv_tree_plan
+  int tile_stride;    // tiles of a table row
+  int2* ends;         // [B][tile_stride]: the largest and the smallest subtree end of a tile
+  int64_t* items;     // costs of the row tiles before each and in all: of sequence b from cu_new[b] / tpt + 2 b on
+  int64_t* seq_cost;  // [B]
 };
 
-template <typename C>
-constexpr int DP_OF = C::DP;
+// What a row tile takes of a tile of keys: 0 nothing (each key's subtree ends before the first row), 2 all of it (every
+// row sees every key), 1 some.
+__device__ __forceinline__ int tile_kind(int2 ends, int last_key, int first, int last) {
+  return ends.x <= first ? 0 : ends.y > last && last_key <= first ? 2 : 1;
+}
 
-template <typename T, typename C>
-__global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 256 ? 2 : 1)) k_kv_attn(KvArgs a, AttnArgs p, AttnPlan pl) {
+// With subtree ends: the line of work counts the tiles of keys that a row tile takes and no others (in a packed tree of
+// many branches fewer than half, and a share that differs by sequence).  Workgroup b: the ends of each of its tiles, then
+// the row tiles' costs, a wavefront to each, and their sums.
+__global__ void __launch_bounds__(1024) k_kv_tree_plan(KvArgs a, AttnArgs p, AttnPlan pl, int TK) {
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const Seq s = sequence(a, b);
+  // (rows that an earlier sequence has too would share its items)
+  int before = 0;
+  for (int i = tid; i < b; i += 1024) before = max(before, a.cu[i]);
+  if (__syncthreads_or(before > s.row0) || s.n == 0) {
+    if (tid == 0) pl.seq_cost[b] = 0;
+    return;
+  }
+  const int* ends = p.slot_end + (int64_t)b * p.end_stride;
+  int2* tiles = pl.ends + (int64_t)b * pl.tile_stride;
+  const int ctx = s.len - s.n, nt = (s.len + TK - 1) / TK;
+  for (int t0 = w; t0 < nt; t0 += 64) {
+    int e[4][2];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int key0 = (t0 + u * 16) * TK + (lane & (TK - 1));
+#pragma unroll
+      for (int k = 0; k < 2; ++k) e[u][k] = ends[min(key0 + (TK > 64 ? k * 64 : 0), s.len - 1)];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      int most = max(e[u][0], e[u][1]), least = min(e[u][0], e[u][1]);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        most = max(most, __shfl_xor(most, o, 64));
+        least = min(least, __shfl_xor(least, o, 64));
+      }
+      if (lane == 0 && t0 + u * 16 < nt) tiles[t0 + u * 16] = make_int2(most, least);
+    }
+  }
+  __syncthreads();
+  const int n_items = (s.n + pl.tpt - 1) / pl.tpt;
+  int64_t* items = pl.items + s.row0 / pl.tpt + 2 * b;
+  for (int i = w; i < n_items; i += 16) {
+    const int first = ctx + i * pl.tpt, last = min(first + pl.tpt, s.len) - 1, kt = last / TK + 1;
+    int n = 0;
+    for (int t0 = 0; t0 < kt; t0 += 64) {
+      const bool takes = t0 + lane < kt && tile_kind(tiles[t0 + lane], 0, first, last) != 0;
+      n += __popcll(__ballot(takes));
+    }
+    if (lane == 0) items[i + 1] = (int64_t)n * TK + kItemCost;
+  }
+  __syncthreads();
+  if (w > 0) return;
+  int64_t sum = 0;
+  if (lane == 0) items[0] = 0;
+  for (int i0 = 0; i0 < n_items; i0 += 64) {
+    int64_t v = i0 + lane < n_items ? items[i0 + lane + 1] : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t u = __shfl_up(v, o, 64);
+      if (lane >= o) v += u;
+    }
+    v += sum;
+    if (i0 + lane < n_items) items[i0 + lane + 1] = v;
+    sum = __shfl(v, 63, 64);
+  }
+  if (lane == 0) pl.seq_cost[b] = sum;
+}
+
+template <typename T, typename C, bool TREE>
+__global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256 ? 2 : 1)) k_kv_attn(KvArgs a, AttnArgs p, AttnPlan pl) {
   typedef typename C::G G;
-  constexpr int ESZ = G::ESZ, EPC = G::EPC, CPR = G::CPR, DP = C::DP, NB = C::NB, NI = C::NI, NS = C::NS, DB = DP / 32;
+  constexpr int ESZ = G::ESZ, EPC = G::EPC, CPR = G::CPR, DP = C::DP, NB = C::NB, NI = C::NI, NS = C::NS, DB = DP / 32, KS = CPR / 2;
   extern __shared__ __align__(1024) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = C::WM > 1 ? wid : 0, kw = C::WK > 1 ? wid : 0;
@@ -247,11 +303,18 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
   int* s_pages = reinterpret_cast<int*>(smem + C::PAGES);
   int* s_ends = reinterpret_cast<int*>(smem + C::ENDS);
   int* s_flag = reinterpret_cast<int*>(smem + C::FLAG);
+  int* s_live = reinterpret_cast<int*>(smem + C::LIVE);
   const int g = a.Hq / a.Hkv, tpt = pl.tpt;
 
   const int nwg = gridDim.x;  // a multiple of 8
   int wg;
   // ---- this workgroup's piece of the line
+  auto seq_cost = [&](int b) {
+    if constexpr (TREE) return pl.seq_cost[b];
+    const Seq s = sequence(a, b);
+    return tiles_cost((s.n + tpt - 1) / tpt, s.len - s.n, tpt);
+  };
+  auto items_of = [&](const Seq& s, int b) { return pl.items + s.row0 / tpt + 2 * b; };
   int64_t tot, piece, lo, hi;
   __shared__ int s_b;
   __shared__ int64_t s_before;
@@ -259,10 +322,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
     const int per = (a.B + C::WAVES * 64 - 1) / (C::WAVES * 64);
     const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
     int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) {
-      const Seq s = sequence(a, b);
-      mine += tiles_cost((s.n + tpt - 1) / tpt, s.len - s.n, tpt);
-    }
+    for (int b = b0; b < b1; ++b) mine += seq_cost(b);
     const int64_t before = block_exclusive<C>(mine, smem, &tot);
     const int64_t all = tot * a.Hkv;
     piece = (all + nwg - 1) / nwg;
@@ -279,8 +339,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
       if (x >= before && x < before + mine) {
         int64_t at = before;
         for (int b = b0; b < b1; ++b) {
-          const Seq s = sequence(a, b);
-          const int64_t c = tiles_cost((s.n + tpt - 1) / tpt, s.len - s.n, tpt);
+          const int64_t c = seq_cost(b);
           if (x < at + c) {
             s_b = b;
             s_before = at;
@@ -305,23 +364,25 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
   int64_t start = h * tot + s_before;  // cost before the sequence; below: before the tile
   int rt = 0;
   {
-    // the tile that holds lo: the last t with tiles_cost(t) <= lo - start
+    // the tile that holds lo: the last with a cost before it <= lo - start
     const int64_t x = lo - start, ctx = s.len - s.n;
+    auto before = [&](int t) { return TREE ? items_of(s, b)[t] : tiles_cost(t, ctx, tpt); };
     int t0 = 0, t1 = (s.n + tpt - 1) / tpt;  // cost(t0) <= x < cost(t1)
     while (t1 - t0 > 1) {
       const int m = (t0 + t1) >> 1;
-      if (tiles_cost(m, ctx, tpt) <= x) t0 = m;
+      if (before(m) <= x) t0 = m;
       else t1 = m;
     }
     rt = t0;
-    start += tiles_cost(t0, ctx, tpt);
+    start += before(t0);
   }
 
   // ---- lane constants
   const int64_t row_bytes = (int64_t)a.D * ESZ;
   const int64_t head_bytes = row_bytes << a.ps_shift, page_bytes = a.Hkv * head_bytes;
   const bool paged_rows = (1 << a.ps_shift) >= G::RPI;  // the rows of a copy lie in one page
-  const int run = min(1 << a.ps_shift, C::LROWS);       // rows of a wavefront's share of a tile that lie in one page
+  // rows of a wavefront's share of a tile that lie in one page
+  const int run = __builtin_amdgcn_readfirstlane(min(1 << a.ps_shift, C::LROWS));
   const int crow = lane / CPR, cchunk = lane % CPR;
   // where a lane's 16 bytes of copy i lie, from the run's first row on: the chunk that its place in LDS holds
   auto copy_offset = [&](int i, bool value) {
@@ -364,17 +425,25 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
     const int ctx = s.len - s.n;
     const int tok0 = rt * tpt, ntok = min(tpt, s.n - tok0);
     const int vis = ctx + tok0 + ntok;
-    const int64_t cost = (int64_t)ctx + (int64_t)(rt + 1) * tpt + kItemCost;
     const int kt = (vis + C::TK - 1) / C::TK;
+    // cost, and tiles to take (with subtree ends k0 and k1 count those alone)
+    int64_t cost = (int64_t)ctx + (int64_t)(rt + 1) * tpt + kItemCost;
+    int takes = kt;
+    if constexpr (TREE) {
+      const int64_t* it = items_of(s, b) + rt;
+      takes = __builtin_amdgcn_readfirstlane((int)(it[1] - it[0] - kItemCost) / C::TK);
+      cost = (int64_t)takes * C::TK + kItemCost;
+    }
     const int64_t x0 = lo > start ? lo - start : 0, x1 = min(hi - start, cost);
-    const int k0 = (int)(x0 * kt / cost), k1 = x1 == cost ? kt : (int)(x1 * kt / cost);
+    const int k0 = (int)(x0 * takes / cost), k1 = x1 == cost ? takes : (int)(x1 * takes / cost);
     const bool whole = x0 == 0 && x1 == cost;
 
     // query rows of this wavefront: token tok0 + row / g, head h g + row % g
     const int row = wm * 32 + ql, rtok = row / g;
     const bool live = rtok < ntok;
     const int qslot = ctx + tok0 + min(rtok, ntok - 1);
-    const int first_slot = ctx + tok0 + min((wm * 32) / g, ntok - 1);       // of the wavefront's rows
+    const int wg_first = ctx + tok0, wg_last = ctx + tok0 + ntok - 1;       // slots of the workgroup's rows
+    const int first_slot = ctx + tok0 + min((wm * 32) / g, ntok - 1);       // of the wavefront's
     const int last_slot = ctx + tok0 + min((wm * 32 + 31) / g, ntok - 1);
     u32x4 qf[CPR / 2];
     {
@@ -398,15 +467,48 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
     float m = -INFINITY, l = 0.0f;
+    float mb = 0.0f, limit = -INFINITY;  // m c (0 before there is one); what mx c may reach without a rescaling
 
     const int64_t head0 = (int64_t)h * head_bytes;
     const int page_keys = kPageCap << a.ps_shift;
-    const int seg_tiles = max(1, page_keys / C::TK);
-    for (int t0 = k0; t0 < k1; t0 += seg_tiles) {
-      const int t1 = min(k1, t0 + seg_tiles);
+    int seg_tiles = max(1, page_keys / C::TK);
+    if constexpr (TREE) seg_tiles = min(seg_tiles, kLiveCap);
+    int seen = 0;  // tiles to take before the segment
+    for (int t0 = TREE ? 0 : k0; TREE ? t0 < kt && seen < k1 && k0 < k1 : t0 < k1; t0 += seg_tiles) {
+      const int t1 = min(TREE ? kt : k1, t0 + seg_tiles);
+      int nt = t1 - t0;
+      __syncthreads();
+      // ---- with subtree ends: the tiles to take, in order, those that every row sees whole marked
+      if constexpr (TREE) {
+        const int2* ends = pl.ends + (int64_t)b * pl.tile_stride + t0;
+        for (int i = tid; i < nt; i += C::WAVES * 64)
+          s_live[i] = tile_kind(ends[i], (t0 + i + 1) * C::TK - 1, wg_first, wg_last);
+        __syncthreads();
+        if (wid == 0) {
+          int n = 0;
+          for (int i0 = 0; i0 < nt; i0 += 64) {
+            const int kind = i0 + lane < nt ? s_live[i0 + lane] : 0;
+            const uint64_t below = (1ull << lane) - 1, who = __ballot(kind != 0);
+            const int nth = seen + __popcll(who & below);
+            const bool mine = kind != 0 && nth >= k0 && nth < k1;
+            const uint64_t taken = __ballot(mine);
+            // never past what is still to be read
+            if (mine) s_live[n + __popcll(taken & below)] = (t0 + i0 + lane) | (kind == 2 ? kWhole : 0);
+            n += __popcll(taken);
+            seen += __popcll(who);
+          }
+          if (lane == 0) {
+            s_live[kLiveCap] = n;
+            s_live[kLiveCap + 1] = seen;
+          }
+        }
+        __syncthreads();
+        nt = __builtin_amdgcn_readfirstlane(s_live[kLiveCap]);
+        seen = __builtin_amdgcn_readfirstlane(s_live[kLiveCap + 1]);
+        if (nt == 0) continue;
+      }
       // ---- page indices of the segment's keys, checked
       const int pg0 = (t0 * C::TK) >> a.ps_shift;
-      __syncthreads();
       {
         const int last = (min(t1 * C::TK, s.len) - 1) >> a.ps_shift;
         for (int i = tid; i < kPageCap; i += C::WAVES * 64) {
@@ -422,6 +524,11 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
         }
       }
       __syncthreads();
+      auto entry = [&](int i) {  // the i-th tile, marked or not; behind them a number that no key belongs to
+        if (i >= nt) return t1;
+        return TREE ? __builtin_amdgcn_readfirstlane(s_live[i]) : t0 + i;
+      };
+      auto tile_at = [&](int i) { return entry(i) & ~kWhole; };
 
       // ---- copies of this wavefront's rows of a tile into a stage
       // (the page indices of a tile are read from LDS a tile before: one lane for each copy)
@@ -429,8 +536,9 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
         const int key = t * C::TK + kw * C::PK + wm * C::LROWS + min(lane, NI - 1) * G::RPI;
         return s_pages[min((key >> a.ps_shift) - pg0, kPageCap - 1)];
       };
-      int pages = pages_of(t0);
-      auto copy_tile = [&](int t, int stage) {
+      int pages = pages_of(tile_at(0));
+      auto copy_tile = [&](int i_tile, int stage) {
+        const int t = tile_at(i_tile);
         const int part0 = t * C::TK + kw * C::PK + wm * C::LROWS;  // first key of the share
         char* dst = smem + stage * C::STAGE + kw * C::PART + wm * C::LROWS * G::ROWB;
         if (paged_rows) {
@@ -461,7 +569,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
               copy(i);
             }
           }
-          pages = pages_of(t + 1);
+          pages = pages_of(tile_at(i_tile + 1));
         } else {
           // pages smaller than a copy's rows: every lane finds its own; rows behind the sequence repeat its last (and a
           // tile behind the segment is whatever, never read)
@@ -483,7 +591,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
             }
           }
         }
-        if (p.slot_end && lane < C::PK) {
+        if (TREE && lane < C::PK) {
           // the same for every wavefront of a row split: each waits for its own copy
           const int key = min(t * C::TK + kw * C::PK + lane, s.len - 1);
           __builtin_amdgcn_global_load_lds(
@@ -494,33 +602,33 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
 
       wait_vmcnt<0>();  // the counts below are of copies alone
 #pragma unroll
-      for (int st = 0; st < NS - 1; ++st) copy_tile(t0 + st, st);
+      for (int st = 0; st < NS - 1; ++st) copy_tile(st, st);
       int stage = 0;
-      for (int t = t0; t < t1; ++t) {
-        const int part0 = t * C::TK + kw * C::PK;
+      for (int it = 0; it < nt; ++it) {
+        const int entry_now = entry(it);
+        const int part0 = (entry_now & ~kWhole) * C::TK + kw * C::PK;
         // the tile that falls NS - 1 further goes where the last one was read; then wait for this one
         if constexpr (C::WM == 1) {
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          copy_tile(t + NS - 1, stage == 0 ? NS - 1 : stage - 1);
-          if (p.slot_end) wait_vmcnt<(NS - 1) * (2 * NI + 1)>();
+          copy_tile(it + NS - 1, stage == 0 ? NS - 1 : stage - 1);
+          if constexpr (TREE) wait_vmcnt<(NS - 1) * (2 * NI + 1)>();
           else wait_vmcnt<(NS - 1) * 2 * NI>();
         } else {
-          if (p.slot_end) wait_vmcnt<(NS - 2) * (2 * NI + 1)>();
+          if constexpr (TREE) wait_vmcnt<(NS - 2) * (2 * NI + 1)>();
           else wait_vmcnt<(NS - 2) * 2 * NI>();
         }
         // What the rows see of the part: nothing (passed over), all of it, or some (masked; and its values are looked
         // through for NaN and infinities, which a zero probability does not keep out of a product).
         bool all_after = true, some_after = true;  // keys whose subtree lasts past the wavefront's last / first slot
-        bool all_wg = true, some_wg = true;        // the same for the workgroup's rows
-        if (p.slot_end) {
+        bool all_wg = true;                        // past the last of the workgroup's rows
+        if (TREE && !(entry_now & kWhole)) {
           const int e = s_ends[stage * C::TK + kw * C::PK + (lane < C::PK ? lane : 0)];
           all_after = __all(e > last_slot);
           some_after = __any(e > first_slot);
-          all_wg = __all(e > ctx + tok0 + ntok - 1);
-          some_wg = __any(e > ctx + tok0);
+          all_wg = __all(e > wg_last);
         }
         const bool active = part0 <= last_slot && some_after;
-        const bool odd_matters = !(part0 + C::PK - 1 <= ctx + tok0 && all_wg) && part0 <= ctx + tok0 + ntok - 1 && some_wg;
+        const bool odd_matters = !(part0 + C::PK - 1 <= wg_first && all_wg) && part0 <= wg_last;
         const char* kst = smem + stage * C::STAGE;
         if (odd_matters) {
           uint32_t odd = 0;
@@ -539,7 +647,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
         }
         if constexpr (C::WM > 1) {
           block_barrier();
-          copy_tile(t + NS - 1, stage == 0 ? NS - 1 : stage - 1);
+          copy_tile(it + NS - 1, stage == 0 ? NS - 1 : stage - 1);
         }
         // this wavefront's share of the tile's values, as pass `pass` takes them
         auto odd_values = [&](int pass) {
@@ -564,7 +672,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
         f32x16 sc[NB];
         if (active) {
           // ---- scores: a group of key fragments ahead of the products
-          constexpr int KS = CPR / 2, GR = ESZ == 2 ? 4 : 2, NG = NB * KS / GR;
+          constexpr int GR = ESZ == 2 ? 4 : 2, NG = NB * KS / GR;
           u32x4 kf[2][GR];
           auto read_k = [&](int i) {
 #pragma unroll
@@ -614,13 +722,16 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
               }
           }
           // ---- running maximum and sum
-          float mx = fmaxf(sc[0][0], sc[NB - 1][15]);  // in C: the compiler waits for the last product here
+          float m0 = sc[0][0], m1 = sc[0][1];
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int r = 0; r < 16; r += 2) mx = max3(mx, sc[nb][r], sc[nb][r + 1]);
-          mx = swap_max(mx);
-          if (__any((mx - m) * c > kLazy || (m == -INFINITY && mx > m))) {
+            for (int r = 0; r < 16; r += 2) {
+              m0 = fmaxf(m0, sc[nb][r]);
+              m1 = fmaxf(m1, sc[nb][r + 1]);
+            }
+          const float mx = swap_max(fmaxf(m0, m1));
+          if (__any(mx * c > limit)) {
             const float m2 = fmaxf(m, mx);
             const float al = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - m2) * c);
             l *= al;
@@ -629,8 +740,9 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
 #pragma unroll
               for (int r = 0; r < 16; ++r) acc[d][r] *= al;
             m = m2;
+            mb = m2 == -INFINITY ? 0.0f : m2 * c;
+            limit = m2 == -INFINITY ? -INFINITY : mb + kLazy;
           }
-          const float mb = m == -INFINITY ? 0.0f : m * c;
           float sum = 0.0f;
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
@@ -652,8 +764,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
               auto step = [&](auto K, auto D0) {
                 constexpr int k = decltype(K)::value, d0 = decltype(D0)::value;
                 u32x4 vf[VB], pf;
-                if constexpr (C::WM > 1) read_v_free<VB, k * 16 * G::ROWB + d0 * 64, 8 * G::ROWB>(u, vf);
-                else read_v<VB, k * 16 * G::ROWB + d0 * 64, 8 * G::ROWB>(u, vf);
+                read_v<VB, k * 16 * G::ROWB + d0 * 64, 8 * G::ROWB>(u, vf);
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
                   pf[w] = pack_bf16x2(sc[k / 2][(k & 1) * 8 + 2 * w], sc[k / 2][(k & 1) * 8 + 2 * w + 1]);
@@ -693,9 +804,9 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
           // the tile once more, for the next part of its values
           if constexpr (C::WM > 1) block_barrier();
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          pages = pages_of(t);
-          copy_tile(t, stage);
-          pages = pages_of(t + NS);
+          pages = pages_of(tile_at(it));
+          copy_tile(it, stage);
+          pages = pages_of(tile_at(it + NS));
           wait_vmcnt<0>();
           odd_values(pass);
           if (pass == 1 && active) {
@@ -805,7 +916,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && DP_OF<C> < 
           ++h;
         }
         s = sequence(a, b);
-      } while (s.n == 0);
+      } while (TREE ? pl.seq_cost[b] == 0 : s.n == 0);
     }
   }
   if (tid == 0) *desc = md;
@@ -919,7 +1030,7 @@ Shape shape(const KvArgs& a, int max_new) {
   return s;
 }
 
-template <typename T, typename C>
+template <typename T, typename C, bool TREE>
 hipError_t run(const KvArgs& a, const AttnArgs& p, const AttnPlan& pl, int wgs, hipStream_t s) {
   static std::once_flag once[64];
   static hipError_t err[64];
@@ -927,30 +1038,38 @@ hipError_t run(const KvArgs& a, const AttnArgs& p, const AttnPlan& pl, int wgs, 
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess || dev < 0 || dev >= 64) return e != hipSuccess ? e : hipErrorInvalidDevice;
   std::call_once(once[dev], [&] {
-    err[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_kv_attn<T, C>), hipFuncAttributeMaxDynamicSharedMemorySize,
+    err[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_kv_attn<T, C, TREE>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                    C::LDS);
   });
   if (err[dev] != hipSuccess) return err[dev];
-  k_kv_attn<T, C><<<wgs, C::WAVES * 64, C::LDS, s>>>(a, p, pl);
+  if constexpr (TREE) k_kv_tree_plan<<<a.B, 1024, 0, s>>>(a, p, pl, C::TK);
+  k_kv_attn<T, C, TREE><<<wgs, C::WAVES * 64, C::LDS, s>>>(a, p, pl);
   constexpr int rows = 256 / (C::DP / 4);
   k_kv_merge<T, C::DP><<<dim3(wgs + 1, (C::BM + rows - 1) / rows), 256, 0, s>>>(a, p, pl, C::BM);
   return hipGetLastError();
 }
 
+template <typename T, int DP>
+hipError_t run_dim(const Shape& sh, const KvArgs& a, const AttnArgs& p, const AttnPlan& pl, hipStream_t s) {
+  if (p.slot_end) return sh.few ? run<T, Few<T, DP>, true>(a, p, pl, sh.wgs, s) : run<T, Many<T, DP>, true>(a, p, pl, sh.wgs, s);
+  return sh.few ? run<T, Few<T, DP>, false>(a, p, pl, sh.wgs, s) : run<T, Many<T, DP>, false>(a, p, pl, sh.wgs, s);
+}
 template <typename T>
 hipError_t run_type(const Shape& sh, const KvArgs& a, const AttnArgs& p, const AttnPlan& pl, hipStream_t s) {
-  if (sh.DP == 64) return sh.few ? run<T, Few<T, 64>>(a, p, pl, sh.wgs, s) : run<T, Many<T, 64>>(a, p, pl, sh.wgs, s);
-  if (sh.DP == 128) return sh.few ? run<T, Few<T, 128>>(a, p, pl, sh.wgs, s) : run<T, Many<T, 128>>(a, p, pl, sh.wgs, s);
-  return sh.few ? run<T, Few<T, 256>>(a, p, pl, sh.wgs, s) : run<T, Many<T, 256>>(a, p, pl, sh.wgs, s);
+  if (sh.DP == 64) return run_dim<T, 64>(sh, a, p, pl, s);
+  if (sh.DP == 128) return run_dim<T, 128>(sh, a, p, pl, s);
+  return run_dim<T, 256>(sh, a, p, pl, s);
 }
 
 constexpr size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 struct Layout {
-  size_t desc, flags, ml, part, total;
+  size_t desc, flags, ml, part, ends, items, seq_cost, total;
 };
-// of the larger of the two shapes: the size does not depend on max_new
-Layout layout(int DP, int wgs, int BM) {
+// The size is of the larger of the two shapes, whatever max_new, and holds the plan of any tree: tiles of 32 keys and,
+// for rows that are more than max_new promised, the least tokens to a row tile.
+Layout layout(const KvArgs& a, int DP, int wgs, int BM) {
   Layout L;
+  const int g = a.Hq / a.Hkv, tpt = g <= 32 ? 32 / g : 128 / g;
   size_t o = up256(sizeof(WsHeader));
   L.desc = o;
   o += up256((size_t)wgs * sizeof(MergeDesc));
@@ -960,18 +1079,24 @@ Layout layout(int DP, int wgs, int BM) {
   o += up256((size_t)wgs * 2 * BM * 8);
   L.part = o;
   o += (size_t)wgs * 2 * BM * DP * 4;
+  L.ends = o;
+  o += up256((size_t)a.B * ((a.cap + 31) / 32) * sizeof(int2));
+  L.items = o;
+  o += up256((size_t)(a.T / tpt + 2 * (int64_t)a.B + 1) * 8);
+  L.seq_cost = o;
+  o += up256((size_t)a.B * 8);
   L.total = o;
   return L;
 }
 
 }  // namespace
 
-size_t kv_attention_workspace(int D) { return layout(padded_dim(D), 512, 128).total; }
+size_t kv_attention_workspace(const KvArgs& a) { return layout(a, padded_dim(a.D), 512, 128).total; }
 
 hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, int max_new, char* ws, hipStream_t s) {
   prof_mark(KK_KV_ATTENTION, true, s);
   const Shape sh = shape(a, max_new);
-  const Layout L = layout(sh.DP, sh.wgs, sh.BM);
+  const Layout L = layout(a, sh.DP, sh.wgs, sh.BM);
   AttnPlan pl = {};
   pl.tpt = sh.tpt;
   pl.min_piece = 128;
@@ -980,6 +1105,10 @@ hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, in
   pl.ml = reinterpret_cast<float2*>(ws + L.ml);
   pl.part = reinterpret_cast<float*>(ws + L.part);
   pl.status = &reinterpret_cast<WsHeader*>(ws)->status;
+  pl.tile_stride = (int)((a.cap + 31) / 32);
+  pl.ends = reinterpret_cast<int2*>(ws + L.ends);
+  pl.items = reinterpret_cast<int64_t*>(ws + L.items);
+  pl.seq_cost = reinterpret_cast<int64_t*>(ws + L.seq_cost);
   const hipError_t e = dtype == RLK_DTYPE_BF16 ? run_type<bf16_t>(sh, a, p, pl, s) : run_type<float>(sh, a, p, pl, s);
   prof_mark(KK_KV_ATTENTION, false, s);
   return e;

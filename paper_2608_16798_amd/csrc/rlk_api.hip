@@ -1116,7 +1116,7 @@ rlk_status_t rlk_kv_workspace_size(const rlk_kv_t* c, size_t* bytes) {
   if (!bytes) return fail(RLK_EINVAL, "bytes is NULL");
   rlk_status_t st = check_kv(c);
   if (st) return st;
-  *bytes = kv_attention_workspace(c->head_dim);
+  *bytes = kv_attention_workspace(kv_args(c));
   return RLK_OK;
 }
 

@@ -307,7 +307,7 @@ struct AttnArgs {
   float* lse;  // may be NULL
 };
 // ---- launchers (k_kv_attn.hip) ----
-size_t kv_attention_workspace(int D);  // header first
+size_t kv_attention_workspace(const KvArgs& a);  // header first
 hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, int max_new, char* ws, hipStream_t s);
 
 // ---- launchers (k_verify.hip) ----
