@@ -100,11 +100,12 @@ struct Geo {
   }
 };
 
-// WM x WK wavefronts: WM groups of 32 query rows, WK groups of 32 NB keys; NS stages of tiles in LDS.
-template <typename T, int DP_, int WM_, int WK_, int NB_, int NS_>
+// WM x WK wavefronts: WM groups of 32 query rows, WK groups of 32 NB keys; NS stages of tiles in LDS.  DC: columns that
+// the products take, the head's rounded up to 32.
+template <typename T, int DP_, int WM_, int WK_, int NB_, int NS_, int DC_ = DP_>
 struct Cfg : Geo<T, DP_> {
   typedef Geo<T, DP_> G;
-  static constexpr int DP = DP_, WM = WM_, WK = WK_, NB = NB_, NS = NS_;
+  static constexpr int DP = DP_, DC = DC_, WM = WM_, WK = WK_, NB = NB_, NS = NS_;
   static constexpr int WAVES = WM * WK, BM = 32 * WM, PK = 32 * NB, TK = PK * WK;  // rows, keys of a part, of a tile
   static constexpr int LROWS = PK / WM, NI = LROWS / G::RPI;                       // a wavefront's share of the copies
   static constexpr int PART = PK * G::ROWB, STAGE = 2 * PART * WK;                 // bytes of K (or V) of a part; of a stage
@@ -121,8 +122,8 @@ struct Cfg : Geo<T, DP_> {
 };
 
 // ds_read_b64_tr_b16: 16 lanes address four rows (lane / 4), 8 bytes each (lane % 4); lane i gets column i of the four.
-// Values of 16 keys (two groups of four per half) for the four or two 32-wide blocks of the head that share the bank
-// pattern: eight (four) reads and their wait in one statement, since the compiler would wait for every copy in flight
+// Values of 16 keys (two groups of four per half) for the two to four 32-wide blocks of the head that share the bank
+// pattern: their reads and their wait in one statement, since the compiler would wait for every copy in flight
 // before a transposing read of its own (it takes the read to alias the copies' LDS writes).
 template <int N, int OFF, int STEP>
 __device__ __forceinline__ void read_v(const int (&u)[N], u32x4 (&f)[N]) {
@@ -136,6 +137,15 @@ __device__ __forceinline__ void read_v(const int (&u)[N], u32x4 (&f)[N]) {
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(l[3]), "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3])
         : "v"(u[0]), "v"(u[1]), "v"(u[2]), "v"(u[3]), "i"(OFF), "i"(OFF + STEP)
+        : "memory");
+  } else if constexpr (N == 3) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %6 offset:%9\n\tds_read_b64_tr_b16 %3, %6 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %1, %7 offset:%9\n\tds_read_b64_tr_b16 %4, %7 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %2, %8 offset:%9\n\tds_read_b64_tr_b16 %5, %8 offset:%10\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2])
+        : "v"(u[0]), "v"(u[1]), "v"(u[2]), "i"(OFF), "i"(OFF + STEP)
         : "memory");
   } else {
     static_assert(N == 2, "blocks of a read");
@@ -295,7 +305,8 @@ __global__ void __launch_bounds__(1024) k_kv_tree_plan(KvArgs a, AttnArgs p, Att
 template <typename T, typename C, bool TREE>
 __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256 ? 2 : 1)) k_kv_attn(KvArgs a, AttnArgs p, AttnPlan pl) {
   typedef typename C::G G;
-  constexpr int ESZ = G::ESZ, EPC = G::EPC, CPR = G::CPR, DP = C::DP, NB = C::NB, NI = C::NI, NS = C::NS, DB = DP / 32, KS = CPR / 2;
+  constexpr int ESZ = G::ESZ, EPC = G::EPC, CPR = G::CPR, DP = C::DP, NB = C::NB, NI = C::NI, NS = C::NS;
+  constexpr int DB = C::DC / 32, KS = C::DC / (2 * EPC);  // 32-wide blocks of the head; steps of two chunks
   extern __shared__ __align__(1024) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = C::WM > 1 ? wid : 0, kw = C::WK > 1 ? wid : 0;
@@ -405,8 +416,8 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256
   };
   // key and value fragments
   const int k_base = kw * C::PART + ql * G::ROWB + ((hl ^ G::k_swz(ql)) << 4);
-  int v_base[DB < 4 ? DB : 4];
   constexpr int VB = DB < 4 ? DB : 4;
+  int v_base[VB];
   {
     const int i = lane & 15, r = i >> 2;
 #pragma unroll
@@ -445,11 +456,11 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256
     const int wg_first = ctx + tok0, wg_last = ctx + tok0 + ntok - 1;       // slots of the workgroup's rows
     const int first_slot = ctx + tok0 + min((wm * 32) / g, ntok - 1);       // of the wavefront's
     const int last_slot = ctx + tok0 + min((wm * 32 + 31) / g, ntok - 1);
-    u32x4 qf[CPR / 2];
+    u32x4 qf[KS];
     {
       const T* q = (const T*)p.q + (int64_t)(s.row0 + tok0 + rtok) * p.q_stride + (int64_t)(h * g + row % g) * a.D;
 #pragma unroll
-      for (int ks = 0; ks < CPR / 2; ++ks) {
+      for (int ks = 0; ks < KS; ++ks) {
         const int e = (2 * ks + hl) * EPC;
         qf[ks] = live && e < a.D ? *reinterpret_cast<const u32x4*>(q + e) : u32x4{0, 0, 0, 0};
         if (sign != 1.0f) {
@@ -672,7 +683,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256
         f32x16 sc[NB];
         if (active) {
           // ---- scores: a group of key fragments ahead of the products
-          constexpr int GR = ESZ == 2 ? 4 : 2, NG = NB * KS / GR;
+          constexpr int GR = ESZ == 4 ? 2 : NB * KS % 4 ? 3 : 4, NG = NB * KS / GR;
           u32x4 kf[2][GR];
           auto read_k = [&](int i) {
 #pragma unroll
@@ -996,18 +1007,22 @@ __global__ void __launch_bounds__(256) k_kv_merge(KvArgs a, AttnArgs p, AttnPlan
 
 // Tiles by type and head size.  Few: 32 query rows, the wavefronts split the keys (one to a few tokens: bound by the
 // cache's bytes).  Many: 128 rows, 32 to a wavefront.
-template <typename T, int DP> struct Few;
-template <typename T, int DP> struct Many;
+template <typename T, int DC> struct Few;
+template <typename T, int DC> struct Many;
 template <> struct Few<bf16_t, 64> : Cfg<bf16_t, 64, 1, 4, 1, 4> {};
+template <> struct Few<bf16_t, 96> : Cfg<bf16_t, 128, 1, 4, 1, 2, 96> {};
 template <> struct Few<bf16_t, 128> : Cfg<bf16_t, 128, 1, 4, 1, 2> {};
 template <> struct Few<bf16_t, 256> : Cfg<bf16_t, 256, 1, 2, 1, 2> {};
 template <> struct Few<float, 64> : Cfg<float, 64, 1, 4, 1, 2> {};
+template <> struct Few<float, 96> : Cfg<float, 128, 1, 2, 1, 2, 96> {};
 template <> struct Few<float, 128> : Cfg<float, 128, 1, 2, 1, 2> {};
 template <> struct Few<float, 256> : Cfg<float, 256, 1, 1, 1, 2> {};
 template <> struct Many<bf16_t, 64> : Cfg<bf16_t, 64, 4, 1, 2, 3> {};
+template <> struct Many<bf16_t, 96> : Cfg<bf16_t, 128, 4, 1, 2, 2, 96> {};
 template <> struct Many<bf16_t, 128> : Cfg<bf16_t, 128, 4, 1, 2, 2> {};
 template <> struct Many<bf16_t, 256> : Cfg<bf16_t, 256, 4, 1, 1, 2> {};
 template <> struct Many<float, 64> : Cfg<float, 64, 4, 1, 1, 2> {};
+template <> struct Many<float, 96> : Cfg<float, 128, 4, 1, 1, 2, 96> {};
 template <> struct Many<float, 128> : Cfg<float, 128, 4, 1, 1, 2> {};
 template <> struct Many<float, 256> : Cfg<float, 256, 4, 1, 1, 2> {};
 
@@ -1049,15 +1064,16 @@ hipError_t run(const KvArgs& a, const AttnArgs& p, const AttnPlan& pl, int wgs, 
   return hipGetLastError();
 }
 
-template <typename T, int DP>
+template <typename T, int DC>
 hipError_t run_dim(const Shape& sh, const KvArgs& a, const AttnArgs& p, const AttnPlan& pl, hipStream_t s) {
-  if (p.slot_end) return sh.few ? run<T, Few<T, DP>, true>(a, p, pl, sh.wgs, s) : run<T, Many<T, DP>, true>(a, p, pl, sh.wgs, s);
-  return sh.few ? run<T, Few<T, DP>, false>(a, p, pl, sh.wgs, s) : run<T, Many<T, DP>, false>(a, p, pl, sh.wgs, s);
+  if (p.slot_end) return sh.few ? run<T, Few<T, DC>, true>(a, p, pl, sh.wgs, s) : run<T, Many<T, DC>, true>(a, p, pl, sh.wgs, s);
+  return sh.few ? run<T, Few<T, DC>, false>(a, p, pl, sh.wgs, s) : run<T, Many<T, DC>, false>(a, p, pl, sh.wgs, s);
 }
 template <typename T>
 hipError_t run_type(const Shape& sh, const KvArgs& a, const AttnArgs& p, const AttnPlan& pl, hipStream_t s) {
-  if (sh.DP == 64) return run_dim<T, 64>(sh, a, p, pl, s);
-  if (sh.DP == 128) return run_dim<T, 128>(sh, a, p, pl, s);
+  if (a.D <= 64) return run_dim<T, 64>(sh, a, p, pl, s);
+  if (a.D <= 96) return run_dim<T, 96>(sh, a, p, pl, s);
+  if (a.D <= 128) return run_dim<T, 128>(sh, a, p, pl, s);
   return run_dim<T, 256>(sh, a, p, pl, s);
 }
 
