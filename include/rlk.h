@@ -349,7 +349,7 @@ rlk_status_t rlk_tree_ends(int32_t R, const int64_t* pos_off, const int32_t* par
  * depth, and rlk_tree_ends says what it sees. */
 typedef struct {
   int64_t T;                  /* rows of q, k, v and of their outputs: the sequences' new tokens back to
-                                 back; rows from cu_new[B] on are left as they were */
+                                 back, at most 2^25; rows from cu_new[B] on are left as they were */
   int32_t B;                  /* sequences, at most 16384 */
   int32_t n_pages;            /* pages of the pools; offsets pass 32 bits */
   int32_t page_size;          /* tokens of a page: a power of two, 1 .. 1024 */
@@ -388,7 +388,9 @@ typedef struct {
 } rlk_rot_t;
 
 /* Workspace bytes of rlk_kv_append and rlk_kv_attention for this cache (one size for both).  Host
- * pointers; device pointers of the descriptor are not read. */
+ * pointers; device pointers of the descriptor are not read.  Besides a fixed part, 8 bytes for every 32
+ * slots of the page table and 8 for every row that attention with slot_end may start a tile at (about
+ * T n_q_heads / (32 n_kv_heads)). */
 rlk_status_t rlk_kv_workspace_size(const rlk_kv_t* c, size_t* bytes);
 
 /* Appends the chunk's keys and values to the cache and makes its queries ready, in one pass: per token,
@@ -429,7 +431,8 @@ rlk_status_t rlk_kv_attention(const rlk_kv_t* c, const void* q, int64_t q_stride
  * (0 elsewhere), which is the log-prob that the loss takes as rollout_logp or old_logp; n_accepted [B].
  * Rows from cu_draft[B] + B on are left as they were.  Logits of -inf have no mass.  Sums and decisions are fp64. */
 typedef struct {
-  int64_t n_draft;     /* rows of draft, u_accept and draft_logits; logits, tokens and logp have n_draft + B */
+  int64_t n_draft;     /* rows of draft, u_accept and draft_logits; logits, tokens and logp have n_draft + B.
+                          (2 n_draft + B) ceil(V / 4096) stays below 2^24 */
   int32_t B;           /* sequences, at most 16384 */
   int32_t V;           /* vocabulary, 1 .. RLK_MAX_DIM */
   int32_t dtype;       /* of both logits */

@@ -367,7 +367,8 @@ rlk_status_t finish(hipError_t e, const char* what, const void* ws, hipStream_t 
 rlk_status_t check_kv(const rlk_kv_t* c) {
   if (!c) return fail(RLK_EINVAL, "cache descriptor is NULL");
   if (c->dtype != RLK_DTYPE_F32 && c->dtype != RLK_DTYPE_BF16) return fail(RLK_EDTYPE, "unknown dtype %d", c->dtype);
-  if (c->T < 0 || c->T >= ((int64_t)1 << 31)) return fail(RLK_ESHAPE, "T = %lld outside [0, 2^31)", (long long)c->T);
+  // (the append's launch has a workgroup of 256 threads to four rows, fewer than 2^32 threads in all)
+  if (c->T < 0 || c->T > kMaxChunkRows) return fail(RLK_ESHAPE, "T = %lld outside [0, %d]", (long long)c->T, kMaxChunkRows);
   if (c->B < 0 || c->B > kMaxRollouts) return fail(RLK_ESHAPE, "B = %d outside [0, %d]", c->B, kMaxRollouts);
   if (c->page_size < 1 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
     return fail(RLK_ESHAPE, "page_size = %d must be a power of two in [1, 1024]", c->page_size);
@@ -433,7 +434,8 @@ rlk_status_t check_verify(const rlk_verify_t* p) {
   if (p->V < 1 || p->V > RLK_MAX_DIM) return fail(RLK_ESHAPE, "V = %d must lie in [1, %d]", p->V, RLK_MAX_DIM);
   if (p->n_draft < 0) return fail(RLK_ESHAPE, "n_draft < 0");
   if (p->B == 0 && p->n_draft != 0) return fail(RLK_ESHAPE, "B = 0 with n_draft = %lld", (long long)p->n_draft);
-  if (p->n_draft >= ((int64_t)1 << 30) || (2 * p->n_draft + p->B) * verify_chunks(p->V) >= ((int64_t)1 << 31))
+  // (a workgroup of 256 threads to every chunk of a row, fewer than 2^32 threads in all)
+  if (p->n_draft >= ((int64_t)1 << 30) || (2 * p->n_draft + p->B) * verify_chunks(p->V) >= ((int64_t)1 << 24))
     return fail(RLK_ESHAPE, "n_draft = %lld rows of V = %d exceed one launch", (long long)p->n_draft, p->V);
   if (p->temperature != 0.0f && !(p->temperature > 0.0f && isfinite(p->temperature)))
     return fail(RLK_EINVAL, "temperature must be 0 (= 1) or finite and > 0");

@@ -73,6 +73,7 @@ inline size_t splitk_bytes(int64_t mmax, int64_t n, const SplitK& p) {
 }
 constexpr int kScanTile = 1024;  // tokens per compaction block
 constexpr int kMaxRollouts = 16384;
+constexpr int kMaxChunkRows = 1 << 25;  // new tokens of one call on a paged cache
 constexpr int kRollSums = 8;     // per-rollout fp64 sums of the loss reduction
 
 // The kinds' numbers are part of the interface: those that no launch marks any more keep their place.

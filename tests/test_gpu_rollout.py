@@ -231,6 +231,79 @@ def test_attention_of_trees(seqs, H, K, D, ps, dtype):
     check_attention(c, table, lens, cu, q, dtype, 1.0 / math.sqrt(D), ends=np.zeros_like(ends), tag="nothing to see")
 
 
+def branches(n, rng, root, mean):
+    """Subtree ends of a root path of `root` positions and branches one after the other behind it, of geometric length."""
+    end = np.full(n, n, np.int64)
+    i = root
+    while i < n:
+        j = min(n, i + int(rng.geometric(1.0 / mean)))
+        end[i:j] = j
+        i = j
+    return end
+
+
+@pytest.mark.parametrize("D", [8, 40, 64, 72, 88, 96, 104, 128, 136, 192])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_head_sizes(D, dtype):
+    """Every width that the products come in and the sizes beside it, for few rows and for many, causal and trees."""
+    for new in (2, 75):
+        c, table, lens, cu, gen = build([(150, new), (0, new)], 2, 16, D, dtype, seed=D)
+        rng = np.random.default_rng(D)
+        q = torch.randn(int(cu[-1]), 4, D, generator=gen, device="cuda").to(DT[dtype])
+        check_attention(c, table, lens, cu, q, dtype, 1.0 / math.sqrt(D), tag=f"D={D} {dtype} new={new}")
+        ends = np.stack([branches(160 + new, rng, 20, 9) for _ in lens])
+        check_attention(c, table, lens, cu, q, dtype, 1.0 / math.sqrt(D), ends=ends, tag="tree")
+
+
+@pytest.mark.parametrize("H,K", [(2, 1), (40, 1), (128, 1)])
+@pytest.mark.parametrize("B", [257, 700])
+def test_attention_of_many_sequences(H, K, B):
+    """More sequences than a workgroup has threads, a third of them without a new token."""
+    rng = np.random.default_rng(B + H)
+    seqs = [(int(rng.integers(0, 40)), int(rng.integers(0, 3))) for _ in range(B)]
+    c, table, lens, cu, gen = build(seqs, K, 8, 16, "bf16", seed=B)
+    q = torch.randn(int(cu[-1]), H, 16, generator=gen, device="cuda").to(torch.bfloat16)
+    check_attention(c, table, lens, cu, q, "bf16", 0.25, tag="causal")
+    ends = np.stack([branches(int(lens.max()), rng, 3, 4) for _ in seqs])
+    for hint in (0, 1):
+        check_attention(c, table, lens, cu, q, "bf16", 0.25, ends=ends, max_new=hint, tag=f"trees, hint {hint}")
+
+
+@pytest.mark.parametrize("ps", [2, 8, 64])
+@pytest.mark.parametrize("new", [3, 70])
+def test_attention_over_long_trees(ps, new):
+    """Histories of more tiles and pages than are looked through at once, seen in part: most branches over, a few keys of
+    a tile, long runs of tiles that no token sees."""
+    rng = np.random.default_rng(ps)
+    seqs = [(36000, new), (9000, new), (5, new)]
+    c, table, lens, cu, gen = build(seqs, 1, ps, 64, "bf16", seed=ps + new)
+    top = int(lens.max())
+    ends = np.stack([branches(top, rng, r, m) for r, m in ((100, 900), (4000, 5), (0, 30))])
+    for b in range(2):  # some long-lived positions among the branches that are over
+        at = rng.integers(0, lens[b] - new, 40)
+        ends[b, at] = top
+    ends[0, 20000:33500] = 20001
+    ends[0, 33300:33400] = top
+    q = torch.randn(int(cu[-1]), 2, 64, generator=gen, device="cuda").to(torch.bfloat16)
+    for hint in (0, 1):
+        check_attention(c, table, lens, cu, q, "bf16", 0.125, ends=ends, max_new=hint, tag=f"hint {hint}")
+    check_attention(c, table, lens, cu, q, "bf16", 0.125, tag="causal")
+
+
+def test_overlapping_rows_of_trees_are_reported():
+    """Offsets that fall back: the sequences that would share rows with an earlier one are left out."""
+    c, table, lens, cu, gen = build([(20, 50), (10, 5), (40, 57)], 2, 16, 64, "bf16", seed=5)
+    q = torch.randn(112, 4, 64, generator=gen, device="cuda").to(torch.bfloat16)
+    ends = torch.full((3, 100), 1000, dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, 7.0)
+    _, _, ws = rlk.kv_attention(q, **dict(c, cu_new=dev([0, 50, 3, 60])), scale=0.125, slot_end=ends, out=out)
+    assert rlk.check_status(ws) == rlk.DERR_CU_SEQLENS
+    ref = RO.kv_attention(host(q), host(c["k_pages"]), host(c["v_pages"]), table[:1], lens[:1], [0, 50], 0.125)
+    x = score_error(ref, 64)[:50]
+    lim = (2.0 ** -8 + 2 * x + 2 * 71 * E + 2.0 ** -20)[..., None] * ref["pv"][:50] + 2.0 ** -8 * np.abs(ref["out"][:50])
+    assert np.all(np.abs(host(out)[:50] - ref["out"][:50]) <= lim) and bool((out[50:] == 7.0).all())
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("dtype,new,D", [("bf16", 5, 128), ("bf16", 90, 64), ("bf16", 90, 256), ("f32", 5, 80), ("f32", 90, 128)])
 def test_unseen_keys_and_values_stay_out(dtype, new, D, bad):
@@ -550,6 +623,43 @@ def test_graph_replay(new):
     torch.cuda.synchronize()
     for n, t in o.items():
         assert torch.equal(t, ref2[n]), n
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured calls of other shapes, one over trees, on one workspace: each replay gives what the call gives."""
+    made, size = [], 0
+    for seed, seqs, D, tree in ((1, [(500, 60), (40, 90)], 64, True), (2, [(900, 1), (3, 2), (70, 1)], 128, False)):
+        c, table, lens, cu, gen = build(seqs, 2, 16, D, "bf16", seed)
+        q = torch.randn(int(cu[-1]), 8, D, generator=gen, device="cuda").to(torch.bfloat16)
+        ends = dev(np.stack([branches(600, np.random.default_rng(b), 30, 40) for b in range(len(seqs))])) if tree else None
+        size = max(size, rlk.kv_workspace_size(rlk.make_cache(**c, T=len(q), n_q_heads=8)))
+        made.append((c, q, ends, torch.empty_like(q), torch.empty(len(q), 8, device="cuda")))
+    ws = rlk.alloc_workspace(size)
+
+    def run(m):
+        rlk.kv_attention(m[1], **m[0], slot_end=m[2], out=m[3], lse=m[4], ws=ws)
+
+    graphs, refs = [], []
+    for m in made:
+        run(m)
+        torch.cuda.synchronize()
+        refs.append((m[3].clone(), m[4].clone()))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run(m)
+        graphs.append(g)
+    for rep in range(4):
+        for m in made:
+            m[3].fill_(7)
+            m[4].fill_(7)
+        for g in graphs if rep % 2 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        assert rlk.check_status(ws) == 0
+        for m, r in zip(made, refs):
+            assert torch.equal(m[3], r[0]) and torch.equal(m[4], r[1]), rep
+        run(made[rep % 2])
+        torch.cuda.synchronize()
 
 
 def test_two_streams():

@@ -159,6 +159,23 @@ def test_append_and_attention_reject():
     assert c_append(None) == EI and c_attend(None) == EI
 
 
+def test_launches_past_2_32_threads_are_refused(monkeypatch):
+    """A workgroup of 256 threads to four tokens (append) or to 4,096 logits (verification)."""
+    lib = rlk.load_library()
+    n = ctypes.c_size_t()
+    c = c_cache()
+    c.T = 1 << 25
+    assert lib.rlk_kv_workspace_size(ctypes.byref(c), ctypes.byref(n)) == rlk.RLK_OK
+    c.T = (1 << 25) + 1
+    assert lib.rlk_kv_workspace_size(ctypes.byref(c), ctypes.byref(n)) == rlk.RLK_ESHAPE
+    p = rlk.Verify(n_draft=0, B=16384, V=4096 * 512, dtype=rlk.DTYPE_BF16, temperature=1.0, ld_logits=4096 * 512, ld_draft=0)
+    assert lib.rlk_verify_workspace_size(ctypes.byref(p), ctypes.byref(n)) == rlk.RLK_OK
+    p.n_draft = 8192  # with the drafts' distributions 2^15 rows of 512 chunks
+    assert lib.rlk_verify_workspace_size(ctypes.byref(p), ctypes.byref(n)) == rlk.RLK_ESHAPE
+    p.n_draft = 8191
+    assert lib.rlk_verify_workspace_size(ctypes.byref(p), ctypes.byref(n)) == rlk.RLK_OK
+
+
 def test_verify_rejects():
     lib = rlk.load_library()
 
