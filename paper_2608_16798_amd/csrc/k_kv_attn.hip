@@ -122,43 +122,73 @@ struct Cfg : Geo<T, DP_> {
 };
 
 // ds_read_b64_tr_b16: 16 lanes address four rows (lane / 4), 8 bytes each (lane % 4); lane i gets column i of the four.
-// Values of 16 keys (two groups of four per half) for the two to four 32-wide blocks of the head that share the bank
-// pattern: their reads and their wait in one statement, since the compiler would wait for every copy in flight
-// before a transposing read of its own (it takes the read to alias the copies' LDS writes).
-template <int N, int OFF, int STEP>
-__device__ __forceinline__ void read_v(const int (&u)[N], u32x4 (&f)[N]) {
-  u32x2 l[N], h[N];
-  if constexpr (N == 4) {
+// Values of S times 16 keys (two groups of four per half, HALF bytes apart; KEYS bytes to the next 16) for the N 32-wide
+// blocks of the head that share the bank pattern: the reads and one wait in one statement, since the compiler would wait
+// for every copy in flight before a transposing read of its own (it takes the read to alias the copies' LDS writes).
+template <int N, int S, int OFF, int HALF, int KEYS>
+__device__ __forceinline__ void read_v(const int (&u)[N], u32x4 (&f)[S][N]) {
+  u32x2 l[S * N], h[S * N];
+  if constexpr (N == 4 && S == 2) {
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %4, %8 offset:%13\n\t"
-        "ds_read_b64_tr_b16 %1, %9 offset:%12\n\tds_read_b64_tr_b16 %5, %9 offset:%13\n\t"
-        "ds_read_b64_tr_b16 %2, %10 offset:%12\n\tds_read_b64_tr_b16 %6, %10 offset:%13\n\t"
-        "ds_read_b64_tr_b16 %3, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %0, %16 offset:%20\n\tds_read_b64_tr_b16 %8, %16 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %1, %17 offset:%20\n\tds_read_b64_tr_b16 %9, %17 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %2, %18 offset:%20\n\tds_read_b64_tr_b16 %10, %18 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %3, %19 offset:%20\n\tds_read_b64_tr_b16 %11, %19 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %4, %16 offset:%22\n\tds_read_b64_tr_b16 %12, %16 offset:%23\n\t"
+        "ds_read_b64_tr_b16 %5, %17 offset:%22\n\tds_read_b64_tr_b16 %13, %17 offset:%23\n\t"
+        "ds_read_b64_tr_b16 %6, %18 offset:%22\n\tds_read_b64_tr_b16 %14, %18 offset:%23\n\t"
+        "ds_read_b64_tr_b16 %7, %19 offset:%22\n\tds_read_b64_tr_b16 %15, %19 offset:%23\n\t"
         "s_waitcnt lgkmcnt(0)"
-        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(l[3]), "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3])
-        : "v"(u[0]), "v"(u[1]), "v"(u[2]), "v"(u[3]), "i"(OFF), "i"(OFF + STEP)
+        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(l[3]), "=&v"(l[4]), "=&v"(l[5]), "=&v"(l[6]), "=&v"(l[7]),
+          "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3]), "=&v"(h[4]), "=&v"(h[5]), "=&v"(h[6]), "=&v"(h[7])
+        : "v"(u[0]), "v"(u[1]), "v"(u[2]), "v"(u[3]), "i"(OFF), "i"(OFF + HALF), "i"(OFF + 1 * KEYS),
+          "i"(OFF + 1 * KEYS + HALF)
         : "memory");
-  } else if constexpr (N == 3) {
+  } else if constexpr (N == 3 && S == 2) {
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %6 offset:%9\n\tds_read_b64_tr_b16 %3, %6 offset:%10\n\t"
-        "ds_read_b64_tr_b16 %1, %7 offset:%9\n\tds_read_b64_tr_b16 %4, %7 offset:%10\n\t"
-        "ds_read_b64_tr_b16 %2, %8 offset:%9\n\tds_read_b64_tr_b16 %5, %8 offset:%10\n\t"
+        "ds_read_b64_tr_b16 %0, %12 offset:%15\n\tds_read_b64_tr_b16 %6, %12 offset:%16\n\t"
+        "ds_read_b64_tr_b16 %1, %13 offset:%15\n\tds_read_b64_tr_b16 %7, %13 offset:%16\n\t"
+        "ds_read_b64_tr_b16 %2, %14 offset:%15\n\tds_read_b64_tr_b16 %8, %14 offset:%16\n\t"
+        "ds_read_b64_tr_b16 %3, %12 offset:%17\n\tds_read_b64_tr_b16 %9, %12 offset:%18\n\t"
+        "ds_read_b64_tr_b16 %4, %13 offset:%17\n\tds_read_b64_tr_b16 %10, %13 offset:%18\n\t"
+        "ds_read_b64_tr_b16 %5, %14 offset:%17\n\tds_read_b64_tr_b16 %11, %14 offset:%18\n\t"
         "s_waitcnt lgkmcnt(0)"
-        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2])
-        : "v"(u[0]), "v"(u[1]), "v"(u[2]), "i"(OFF), "i"(OFF + STEP)
+        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(l[3]), "=&v"(l[4]), "=&v"(l[5]), "=&v"(h[0]), "=&v"(h[1]),
+          "=&v"(h[2]), "=&v"(h[3]), "=&v"(h[4]), "=&v"(h[5])
+        : "v"(u[0]), "v"(u[1]), "v"(u[2]), "i"(OFF), "i"(OFF + HALF), "i"(OFF + 1 * KEYS), "i"(OFF + 1 * KEYS + HALF)
+        : "memory");
+  } else if constexpr (N == 2 && S == 4) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %16 offset:%18\n\tds_read_b64_tr_b16 %8, %16 offset:%19\n\t"
+        "ds_read_b64_tr_b16 %1, %17 offset:%18\n\tds_read_b64_tr_b16 %9, %17 offset:%19\n\t"
+        "ds_read_b64_tr_b16 %2, %16 offset:%20\n\tds_read_b64_tr_b16 %10, %16 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %3, %17 offset:%20\n\tds_read_b64_tr_b16 %11, %17 offset:%21\n\t"
+        "ds_read_b64_tr_b16 %4, %16 offset:%22\n\tds_read_b64_tr_b16 %12, %16 offset:%23\n\t"
+        "ds_read_b64_tr_b16 %5, %17 offset:%22\n\tds_read_b64_tr_b16 %13, %17 offset:%23\n\t"
+        "ds_read_b64_tr_b16 %6, %16 offset:%24\n\tds_read_b64_tr_b16 %14, %16 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %7, %17 offset:%24\n\tds_read_b64_tr_b16 %15, %17 offset:%25\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(l[3]), "=&v"(l[4]), "=&v"(l[5]), "=&v"(l[6]), "=&v"(l[7]),
+          "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3]), "=&v"(h[4]), "=&v"(h[5]), "=&v"(h[6]), "=&v"(h[7])
+        : "v"(u[0]), "v"(u[1]), "i"(OFF), "i"(OFF + HALF), "i"(OFF + 1 * KEYS), "i"(OFF + 1 * KEYS + HALF),
+          "i"(OFF + 2 * KEYS), "i"(OFF + 2 * KEYS + HALF), "i"(OFF + 3 * KEYS), "i"(OFF + 3 * KEYS + HALF)
         : "memory");
   } else {
-    static_assert(N == 2, "blocks of a read");
+    static_assert(N == 2 && S == 2, "blocks and steps of a read");
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %2, %4 offset:%7\n\t"
-        "ds_read_b64_tr_b16 %1, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+        "ds_read_b64_tr_b16 %0, %8 offset:%10\n\tds_read_b64_tr_b16 %4, %8 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %1, %9 offset:%10\n\tds_read_b64_tr_b16 %5, %9 offset:%11\n\t"
+        "ds_read_b64_tr_b16 %2, %8 offset:%12\n\tds_read_b64_tr_b16 %6, %8 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %3, %9 offset:%12\n\tds_read_b64_tr_b16 %7, %9 offset:%13\n\t"
         "s_waitcnt lgkmcnt(0)"
-        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(h[0]), "=&v"(h[1])
-        : "v"(u[0]), "v"(u[1]), "i"(OFF), "i"(OFF + STEP)
+        : "=&v"(l[0]), "=&v"(l[1]), "=&v"(l[2]), "=&v"(l[3]), "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3])
+        : "v"(u[0]), "v"(u[1]), "i"(OFF), "i"(OFF + HALF), "i"(OFF + 1 * KEYS), "i"(OFF + 1 * KEYS + HALF)
         : "memory");
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) f[i] = u32x4{l[i].x, l[i].y, h[i].x, h[i].y};
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[s][i] = u32x4{l[s * N + i].x, l[s * N + i].y, h[s * N + i].x, h[s * N + i].y};
 }
 
 // Values of a tile that holds infinities or NaN, where some row does not see every key (a zero probability times one of
@@ -681,6 +711,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256
           if (poisoned) odd_values(0);
         }
         f32x16 sc[NB];
+        u32x4 pw[2 * NB];  // bf16: the probabilities, 16 keys to an element
         if (active) {
           // ---- scores: a group of key fragments ahead of the products
           constexpr int GR = ESZ == 4 ? 2 : NB * KS % 4 ? 3 : 4, NG = NB * KS / GR;
@@ -763,6 +794,13 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256
               sum += sc[nb][r];
             }
           l += sum;
+          if constexpr (ESZ == 2) {
+#pragma unroll
+            for (int k = 0; k < 2 * NB; ++k)
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+                pw[k][w] = pack_bf16x2(sc[k / 2][(k & 1) * 8 + 2 * w], sc[k / 2][(k & 1) * 8 + 2 * w + 1]);
+          }
         }
         // ---- values
         for (int pass = 0;;) {
@@ -771,28 +809,25 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256
               int u[VB];
 #pragma unroll
               for (int d = 0; d < VB; ++d) u[d] = v_base[d] + stage * C::STAGE;
-              // 16 keys and up to four 32-wide blocks of the head
-              auto step = [&](auto K, auto D0) {
+              // 32 (64) keys and up to four (two) 32-wide blocks of the head
+              constexpr int S = VB == 2 && NB == 2 ? 4 : 2;
+              auto steps = [&](auto K, auto D0) {
                 constexpr int k = decltype(K)::value, d0 = decltype(D0)::value;
-                u32x4 vf[VB], pf;
-                read_v<VB, k * 16 * G::ROWB + d0 * 64, 8 * G::ROWB>(u, vf);
+                u32x4 vf[S][VB];
+                read_v<VB, S, k * 16 * G::ROWB + d0 * 64, 8 * G::ROWB, 16 * G::ROWB>(u, vf);
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
-                  pf[w] = pack_bf16x2(sc[k / 2][(k & 1) * 8 + 2 * w], sc[k / 2][(k & 1) * 8 + 2 * w + 1]);
+                for (int s = 0; s < S; ++s)
 #pragma unroll
-                for (int d = 0; d < VB; ++d)
-                  acc[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d]),
-                                                                        __builtin_bit_cast(bf16x8, pf), acc[d0 + d], 0, 0, 0);
+                  for (int d = 0; d < VB; ++d)
+                    acc[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[s][d]),
+                                                                          __builtin_bit_cast(bf16x8, pw[k + s]), acc[d0 + d], 0,
+                                                                          0, 0);
               };
-              auto steps = [&](auto K) {
-                step(K, std::integral_constant<int, 0>{});
-                if constexpr (DB > 4) step(K, std::integral_constant<int, 4>{});
-              };
-              steps(std::integral_constant<int, 0>{});
-              steps(std::integral_constant<int, 1>{});
-              if constexpr (NB > 1) {
-                steps(std::integral_constant<int, 2>{});
-                steps(std::integral_constant<int, 3>{});
+              steps(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+              if constexpr (DB > 4) steps(std::integral_constant<int, 0>{}, std::integral_constant<int, 4>{});
+              if constexpr (2 * NB > S) {
+                steps(std::integral_constant<int, 2>{}, std::integral_constant<int, 0>{});
+                if constexpr (DB > 4) steps(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
               }
             } else {
               const char* v0 = kst + (C::WK + kw) * C::PART;
@@ -812,20 +847,30 @@ __global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256
             }
           }
           if (__builtin_expect(!poisoned, 1) || ++pass == 3) break;
-          // the tile once more, for the next part of its values
+          // the tile once more, for the next part of its values (it and stage by way of a statement that the compiler does
+          // not see through: it would prepare this copy for every tile)
+          int again = it, into = stage;
+          asm volatile("" : "+s"(again), "+s"(into));
           if constexpr (C::WM > 1) block_barrier();
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          pages = pages_of(tile_at(it));
-          copy_tile(it, stage);
-          pages = pages_of(tile_at(it + NS));
+          pages = pages_of(tile_at(again));
+          copy_tile(again, into);
+          pages = pages_of(tile_at(again + NS));
           wait_vmcnt<0>();
           odd_values(pass);
           if (pass == 1 && active) {
-            const float most = ESZ == 2 ? 3.3895314e38f : 3.4028235e38f;
+            // the largest number where there is a probability
+            if constexpr (ESZ == 2) {
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+              for (int k = 0; k < 2 * NB; ++k)
 #pragma unroll
-              for (int r = 0; r < 16; ++r) sc[nb][r] = sc[nb][r] > 0.0f ? most : 0.0f;
+                for (int w = 0; w < 4; ++w) pw[k][w] = (((pw[k][w] + 0x7fff7fffu) & 0x80008000u) >> 15) * 0x7f7fu;
+            } else {
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sc[nb][r] = sc[nb][r] > 0.0f ? 3.4028235e38f : 0.0f;
+            }
           }
         }
         stage = stage + 1 == NS ? 0 : stage + 1;
