@@ -100,12 +100,13 @@ struct Geo {
   }
 };
 
-// WM x WK wavefronts: WM groups of 32 query rows, WK groups of 32 NB keys; NS stages of tiles in LDS.  DC: columns that
-// the products take, the head's rounded up to 32.
-template <typename T, int DP_, int WM_, int WK_, int NB_, int NS_, int DC_ = DP_>
+// WM x WK wavefronts: WM groups of 32 query rows, WK groups of 32 NB keys; NS stages of tiles in LDS.  OCC:
+// wavefronts of a SIMD that the registers are shared out for.  DC: columns that the products take, the head's rounded up
+// to 32.
+template <typename T, int DP_, int WM_, int WK_, int NB_, int NS_, int OCC_, int DC_ = DP_>
 struct Cfg : Geo<T, DP_> {
   typedef Geo<T, DP_> G;
-  static constexpr int DP = DP_, DC = DC_, WM = WM_, WK = WK_, NB = NB_, NS = NS_;
+  static constexpr int DP = DP_, DC = DC_, WM = WM_, WK = WK_, NB = NB_, NS = NS_, OCC = OCC_;
   static constexpr int WAVES = WM * WK, BM = 32 * WM, PK = 32 * NB, TK = PK * WK;  // rows, keys of a part, of a tile
   static constexpr int LROWS = PK / WM, NI = LROWS / G::RPI;                       // a wavefront's share of the copies
   static constexpr int PART = PK * G::ROWB, STAGE = 2 * PART * WK;                 // bytes of K (or V) of a part; of a stage
@@ -333,7 +334,7 @@ __global__ void __launch_bounds__(1024) k_kv_tree_plan(KvArgs a, AttnArgs p, Att
 }
 
 template <typename T, typename C, bool TREE>
-__global__ void __launch_bounds__(C::WAVES * 64, (C::LDS <= 81920 && C::DP < 256 ? 2 : 1)) k_kv_attn(KvArgs a, AttnArgs p, AttnPlan pl) {
+__global__ void __launch_bounds__(C::WAVES * 64, C::OCC) k_kv_attn(KvArgs a, AttnArgs p, AttnPlan pl) {
   typedef typename C::G G;
   constexpr int ESZ = G::ESZ, EPC = G::EPC, CPR = G::CPR, DP = C::DP, NB = C::NB, NI = C::NI, NS = C::NS;
   constexpr int DB = C::DC / 32, KS = C::DC / (2 * EPC);  // 32-wide blocks of the head; steps of two chunks
@@ -1054,22 +1055,22 @@ __global__ void __launch_bounds__(256) k_kv_merge(KvArgs a, AttnArgs p, AttnPlan
 // cache's bytes).  Many: 128 rows, 32 to a wavefront.
 template <typename T, int DC> struct Few;
 template <typename T, int DC> struct Many;
-template <> struct Few<bf16_t, 64> : Cfg<bf16_t, 64, 1, 4, 1, 4> {};
-template <> struct Few<bf16_t, 96> : Cfg<bf16_t, 128, 1, 4, 1, 2, 96> {};
-template <> struct Few<bf16_t, 128> : Cfg<bf16_t, 128, 1, 4, 1, 2> {};
-template <> struct Few<bf16_t, 256> : Cfg<bf16_t, 256, 1, 2, 1, 2> {};
-template <> struct Few<float, 64> : Cfg<float, 64, 1, 4, 1, 2> {};
-template <> struct Few<float, 96> : Cfg<float, 128, 1, 2, 1, 2, 96> {};
-template <> struct Few<float, 128> : Cfg<float, 128, 1, 2, 1, 2> {};
-template <> struct Few<float, 256> : Cfg<float, 256, 1, 1, 1, 2> {};
-template <> struct Many<bf16_t, 64> : Cfg<bf16_t, 64, 4, 1, 2, 3> {};
-template <> struct Many<bf16_t, 96> : Cfg<bf16_t, 128, 4, 1, 2, 2, 96> {};
-template <> struct Many<bf16_t, 128> : Cfg<bf16_t, 128, 4, 1, 2, 2> {};
-template <> struct Many<bf16_t, 256> : Cfg<bf16_t, 256, 4, 1, 1, 2> {};
-template <> struct Many<float, 64> : Cfg<float, 64, 4, 1, 1, 2> {};
-template <> struct Many<float, 96> : Cfg<float, 128, 4, 1, 1, 2, 96> {};
-template <> struct Many<float, 128> : Cfg<float, 128, 4, 1, 1, 2> {};
-template <> struct Many<float, 256> : Cfg<float, 256, 4, 1, 1, 2> {};
+template <> struct Few<bf16_t, 64> : Cfg<bf16_t, 64, 1, 4, 1, 4, 1> {};
+template <> struct Few<bf16_t, 96> : Cfg<bf16_t, 128, 1, 4, 1, 2, 1, 96> {};
+template <> struct Few<bf16_t, 128> : Cfg<bf16_t, 128, 1, 4, 1, 2, 1> {};
+template <> struct Few<bf16_t, 256> : Cfg<bf16_t, 256, 1, 2, 1, 2, 1> {};
+template <> struct Few<float, 64> : Cfg<float, 64, 1, 4, 1, 2, 1> {};
+template <> struct Few<float, 96> : Cfg<float, 128, 1, 2, 1, 2, 1, 96> {};
+template <> struct Few<float, 128> : Cfg<float, 128, 1, 2, 1, 2, 1> {};
+template <> struct Few<float, 256> : Cfg<float, 256, 1, 1, 1, 2, 1> {};
+template <> struct Many<bf16_t, 64> : Cfg<bf16_t, 64, 4, 1, 2, 2, 3> {};
+template <> struct Many<bf16_t, 96> : Cfg<bf16_t, 128, 4, 1, 2, 2, 2, 96> {};
+template <> struct Many<bf16_t, 128> : Cfg<bf16_t, 128, 4, 1, 2, 2, 2> {};
+template <> struct Many<bf16_t, 256> : Cfg<bf16_t, 256, 4, 1, 1, 2, 1> {};
+template <> struct Many<float, 64> : Cfg<float, 64, 4, 1, 1, 2, 2> {};
+template <> struct Many<float, 96> : Cfg<float, 128, 4, 1, 1, 2, 2, 96> {};
+template <> struct Many<float, 128> : Cfg<float, 128, 4, 1, 1, 2, 2> {};
+template <> struct Many<float, 256> : Cfg<float, 256, 4, 1, 1, 2, 1> {};
 
 constexpr int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
@@ -1078,7 +1079,7 @@ struct Shape {
   bool few;
   int DP, BM, tpt, wgs;
 };
-Shape shape(const KvArgs& a, int max_new) {
+Shape shape(const KvArgs& a, bool bf16, int max_new) {
   Shape s;
   const int g = a.Hq / a.Hkv;
   const int64_t most = max_new > 0 ? std::min<int64_t>(max_new, a.T) : a.T;
@@ -1086,7 +1087,7 @@ Shape shape(const KvArgs& a, int max_new) {
   s.few = g <= 32 && most * g <= 32;
   s.BM = s.few ? 32 : 128;
   s.tpt = s.BM / g;
-  s.wgs = s.few ? 256 : 512;
+  s.wgs = s.few ? 256 : bf16 && s.DP == 64 ? 768 : 512;
   return s;
 }
 
@@ -1152,11 +1153,11 @@ Layout layout(const KvArgs& a, int DP, int wgs, int BM) {
 
 }  // namespace
 
-size_t kv_attention_workspace(const KvArgs& a) { return layout(a, padded_dim(a.D), 512, 128).total; }
+size_t kv_attention_workspace(const KvArgs& a) { return layout(a, padded_dim(a.D), 768, 128).total; }
 
 hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, int max_new, char* ws, hipStream_t s) {
   prof_mark(KK_KV_ATTENTION, true, s);
-  const Shape sh = shape(a, max_new);
+  const Shape sh = shape(a, dtype == RLK_DTYPE_BF16, max_new);
   const Layout L = layout(a, sh.DP, sh.wgs, sh.BM);
   AttnPlan pl = {};
   pl.tpt = sh.tpt;
