@@ -429,7 +429,8 @@ rlk_status_t rlk_kv_attention(const rlk_kv_t* c, const void* q, int64_t q_stride
  * (in token order) exceeds u_sample[b] times the whole.
  * Outputs by row: tokens (accepted drafts, then the drawn token, then -1) and logp, log p of each emitted token
  * (0 elsewhere), which is the log-prob that the loss takes as rollout_logp or old_logp; n_accepted [B].
- * Rows from cu_draft[B] + B on are left as they were.  Logits of -inf have no mass.  Sums and decisions are fp64. */
+ * Rows from cu_draft[B] + B on are left as they were.  Logits of -inf have no mass, nor have those
+ * below 2^-999 of the largest.  Sums and decisions are fp64. */
 typedef struct {
   int64_t n_draft;     /* rows of draft, u_accept and draft_logits; logits, tokens and logp have n_draft + B.
                           (2 n_draft + B) ceil(V / 4096) stays below 2^24 */

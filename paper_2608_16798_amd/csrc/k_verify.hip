@@ -18,6 +18,7 @@ namespace rlk {
 namespace {
 
 constexpr int kChunk = 4096;  // tokens of a chunk: 16 to a thread
+constexpr int kDrawThreads = 512;  // of the draw, where few workgroups run: half the tokens and sums of a chunk to a thread
 
 struct Part {
   double s;  // sum of exp((z - m) / tau) over the chunk
@@ -103,9 +104,10 @@ __device__ __forceinline__ double mass_of(float z, double c, double b, const dou
   const double t = fma((double)z, c, b);
   return t < -31968.0 ? 0.0 : pow2(t, tab);
 }
-// a chunk's sum against the row's largest logit
+// a chunk's sum against the row's largest logit: above 0 exactly where the chunk's largest logit has mass
 __device__ __forceinline__ double rescaled(double s, double m, double row_m, double c, const double* tab) {
-  return m == -INFINITY ? s : s * pow2((m - row_m) * c, tab);
+  const double t = fma(m, c, -row_m * c);
+  return m == -INFINITY ? s : t < -31968.0 ? s * 0.0 : s * pow2(t, tab);  // (NaN stays)
 }
 
 // Maximum of three, of a number and a NaN the number.  (fmaxf quiets every operand first: one instruction more for each
@@ -320,10 +322,10 @@ __global__ void __launch_bounds__(256) k_verify_decide(VerifyArgs a, const Part*
   }
 }
 
-// N inclusive sums over the workgroup's 256 threads at once, each behind the one before it: v[i] becomes the sum over
+// N inclusive sums over the workgroup's 64 W threads at once, each behind the one before it: v[i] becomes the sum over
 // the whole of v[0 .. i - 1] and the threads up to this one of v[i].  Returns the whole.
-template <int N>
-__device__ __forceinline__ double block_scan(double (&v)[N], double (*s_w)[4]) {
+template <int N, int W>
+__device__ __forceinline__ double block_scan(double (&v)[N], double (*s_w)[W]) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1)
@@ -341,46 +343,58 @@ __device__ __forceinline__ double block_scan(double (&v)[N], double (*s_w)[4]) {
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < W; ++k) {
       if (k == w) v[i] += base;
       base += s_w[i][k];
     }
   return base;
 }
 
+// The lowest lane with a `hit` and the highest with `any`, the only ones that could count, bring their numbers: `at` and
+// `to` grow with the lane.
+__device__ __forceinline__ void first_and_last(bool hit, int at, bool any, int to, int* first, int* last) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t h = __ballot(hit), n = __ballot(any);
+  if (h && lane == __ffsll((unsigned long long)h) - 1) atomicMin(first, at);
+  if (n && lane == 63 - __clzll((long long)n)) atomicMax(last, to);
+}
+
 // One workgroup per sequence: the chunk whose running mass passes the target, then the token in it.
 template <typename T>
-__global__ void __launch_bounds__(256) k_verify_draw(VerifyArgs a, const Part* part, const double* mass,
+__global__ void __launch_bounds__(kDrawThreads) k_verify_draw(VerifyArgs a, const Part* part, const double* mass,
                                                      const Choice* choice) {
-  constexpr int E = 16 / (int)sizeof(T), I = kChunk / (256 * E);
-  constexpr int M = (RLK_MAX_DIM / kChunk + 255) / 256;  // most chunks of a thread
+  constexpr int E = 16 / (int)sizeof(T), I = kChunk / (kDrawThreads * E);
+  constexpr int M = (RLK_MAX_DIM / kChunk + kDrawThreads - 1) / kDrawThreads;  // most chunks of a thread
   const int b = blockIdx.x, tid = threadIdx.x;
+  // what does not depend on the choice is on its way with it
   const Choice ch = choice[b];
+  const double* mb = mass + (int64_t)b * a.nchunk;
+  double v[M], cum[M], total = 0.0;
+#pragma unroll
+  for (int i = 0; i < M; ++i) v[i] = i * kDrawThreads + tid < a.nchunk ? mb[i * kDrawThreads + tid] : 0.0;
+  const int64_t d0 = a.cu[b], r0 = d0 + b;
+  const double u = (double)a.u_sample[b];
   if (ch.acc < 0) return;
-  __shared__ double s_w[I > M ? I : M][4];
+  __shared__ double s_w[I > M ? I : M][kDrawThreads / 64];
   __shared__ int s_first, s_last, s_pick, s_any;
   __shared__ double s_before, s_tab[32];
   load_table(s_tab);
   __syncthreads();
-  const int64_t d0 = a.cu[b], r0 = d0 + b;
-  const double* mb = mass + (int64_t)b * a.nchunk;
   const Part* pb = part + (r0 + ch.acc) * a.nchunk;
   bool residual = ch.residual != 0;
-  double v[M], cum[M], total = 0.0;
   for (;;) {
 #pragma unroll
-    for (int i = 0; i < M; ++i) {
-      const int c = i * 256 + tid;
-      v[i] = 0.0;
-      if (c < a.nchunk)
-        v[i] = residual || !ch.residual ? mb[c] : rescaled(pb[c].s, pb[c].m, ch.pm, a.c, s_tab) / ch.ps;
-      cum[i] = v[i];
-    }
+    for (int i = 0; i < M; ++i) cum[i] = v[i];
     total = block_scan(cum, s_w);
     if (total > 0.0 || !residual) break;
     residual = false;  // nothing left over: drawn from p
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      const int c = i * kDrawThreads + tid;
+      v[i] = c < a.nchunk ? rescaled(pb[c].s, pb[c].m, ch.pm, a.c, s_tab) / ch.ps : 0.0;
+    }
   }
-  const double target = (double)a.u_sample[b] * total;
+  const double target = u * total;
   if (tid == 0) {
     s_pick = INT_MAX;
     s_any = 0;
@@ -390,26 +404,26 @@ __global__ void __launch_bounds__(256) k_verify_draw(VerifyArgs a, const Part* p
   __syncthreads();
   // the first chunk whose running sum passes the target; failing that (u of 1, rounding) the last with mass
 #pragma unroll
-  for (int i = 0; i < M; ++i)
-    if (v[i] > 0.0) {
-      atomicMax(&s_any, i * 256 + tid);
-      if (cum[i] > target) atomicMin(&s_pick, i * 256 + tid);
-    }
+  for (int i = 0; i < M; ++i) {
+    const int c = i * kDrawThreads + tid;
+    first_and_last(v[i] > 0.0 && cum[i] > target, c, v[i] > 0.0, c, &s_pick, &s_any);
+  }
   __syncthreads();
   const int pick = s_pick < INT_MAX ? s_pick : s_any;
 #pragma unroll
   for (int i = 0; i < M; ++i)
-    if (i * 256 + tid == pick) s_before = cum[i] - v[i];
+    if (i * kDrawThreads + tid == pick) s_before = cum[i] - v[i];
   const T* zp = (const T*)a.logits + (r0 + ch.acc) * a.ld_logits;
   const T* zq = residual && a.draft_logits ? (const T*)a.draft_logits + (d0 + ch.acc) * a.ld_draft : nullptr;
   const int y = residual && !a.draft_logits ? a.draft[d0 + ch.acc] : -1;
   const double bp = -ch.pm * a.c, bq = -ch.qm * a.c, np = 1.0 / ch.ps, nq = 1.0 / ch.qs;
   float x[I][E], xq[I][E];
   double t[I][E], sum[I];
+  const double log_s = log(ch.ps);
 #pragma unroll
   for (int i = 0; i < I; ++i) {
-    load_logits(zp, pick * kChunk + (i * 256 + tid) * E, a.V, x[i]);
-    if (zq) load_logits(zq, pick * kChunk + (i * 256 + tid) * E, a.V, xq[i]);
+    load_logits(zp, pick * kChunk + (i * kDrawThreads + tid) * E, a.V, x[i]);
+    if (zq) load_logits(zq, pick * kChunk + (i * kDrawThreads + tid) * E, a.V, xq[i]);
   }
 #pragma unroll
   for (int i = 0; i < I; ++i) {
@@ -418,7 +432,7 @@ __global__ void __launch_bounds__(256) k_verify_draw(VerifyArgs a, const Part* p
     for (int e = 0; e < E; ++e) {
       t[i][e] = mass_of(x[i][e], a.c, bp, s_tab) * np;
       if (zq) t[i][e] = fmax(t[i][e] - mass_of(xq[i][e], a.c, bq, s_tab) * nq, 0.0);
-      if (pick * kChunk + (i * 256 + tid) * E + e == y) t[i][e] = 0.0;
+      if (pick * kChunk + (i * kDrawThreads + tid) * E + e == y) t[i][e] = 0.0;
       sum[i] += t[i][e];
     }
   }
@@ -427,31 +441,33 @@ __global__ void __launch_bounds__(256) k_verify_draw(VerifyArgs a, const Part* p
   for (int i = 0; i < I; ++i) upto[i] = sum[i];
   block_scan(upto, s_w);  // its barriers also order s_before
   const double before = s_before;
-  int first = INT_MAX, last = -1;
 #pragma unroll
   for (int i = 0; i < I; ++i) {
+    int first = INT_MAX, last = -1;
     double run = before + (upto[i] - sum[i]);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       run += t[i][e];
-      const int at = pick * kChunk + (i * 256 + tid) * E + e;
+      const int at = pick * kChunk + (i * kDrawThreads + tid) * E + e;
       if (t[i][e] > 0.0) {
         last = at;
         if (run > target) first = min(first, at);
       }
     }
+    first_and_last(first < INT_MAX, first, last >= 0, last, &s_first, &s_last);
   }
-  if (first < INT_MAX) atomicMin(&s_first, first);
-  if (last >= 0) atomicMax(&s_last, last);
   __syncthreads();
-  if (tid == 0) {
-    const int tok = s_first < INT_MAX ? s_first : s_last;
-    const int64_t r = r0 + ch.acc;
-    a.tokens[r] = tok;
-    a.logp[r] = tok < 0 ? 0.0f
-                        : (float)(((double)load_logit((const T*)a.logits + r * a.ld_logits, tok) - ch.pm) * a.inv_tau -
-                                  log(ch.ps));
-  }
+  // (there is a token: the chunk has mass)
+  const int tok = s_first < INT_MAX ? s_first : s_last;
+  const int64_t r = r0 + ch.acc;
+#pragma unroll
+  for (int i = 0; i < I; ++i)
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (pick * kChunk + (i * kDrawThreads + tid) * E + e == tok) {
+        a.tokens[r] = tok;
+        a.logp[r] = (float)(((double)x[i][e] - ch.pm) * a.inv_tau - log_s);
+      }
 }
 
 }  // namespace
@@ -474,11 +490,11 @@ hipError_t launch_draft_verify(int dtype, const VerifyArgs& a, void* part, doubl
   if (dtype == RLK_DTYPE_BF16) {
     k_verify_stats<bf16_t><<<grid, 256, 0, s>>>(a, pt, status);
     k_verify_decide<bf16_t><<<grid2, 256, 0, s>>>(a, pt, mass, ch, per, status);
-    k_verify_draw<bf16_t><<<(unsigned)a.B, 256, 0, s>>>(a, pt, mass, ch);
+    k_verify_draw<bf16_t><<<(unsigned)a.B, kDrawThreads, 0, s>>>(a, pt, mass, ch);
   } else {
     k_verify_stats<float><<<grid, 256, 0, s>>>(a, pt, status);
     k_verify_decide<float><<<grid2, 256, 0, s>>>(a, pt, mass, ch, per, status);
-    k_verify_draw<float><<<(unsigned)a.B, 256, 0, s>>>(a, pt, mass, ch);
+    k_verify_draw<float><<<(unsigned)a.B, kDrawThreads, 0, s>>>(a, pt, mass, ch);
   }
   prof_mark(KK_VERIFY, false, s);
   return hipGetLastError();

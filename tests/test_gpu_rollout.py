@@ -532,6 +532,27 @@ def test_verify_random_numbers_of_one_and_rows_behind_the_last():
     assert rlk.check_status(ws) == 0 and int(tok[6]) == 77 and float(logp[6]) == 7.0
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_verify_masses_that_vanish(dtype):
+    """Stretches of a row that hold no mass, -inf or far below the largest logit, are never drawn from; NaN is found
+    among them."""
+    V = 9000
+    z = torch.full((3, V), -1e4, dtype=DT[dtype], device="cuda")
+    z[:, 4100:4110] = 1.0
+    z[1, 5000:] = -float("inf")
+    z[2, :4096] = -float("inf")
+    z[2, 4200:] = -300.0  # little, but some: 2^-434 of the largest
+    a = dict(logits=z, draft=dev([]), cu_draft=dev([0, 0, 0, 0]), u_accept=torch.empty(0, device="cuda"))
+    for u, want in ((0.0, [4100, 4100, 4100]), (0.55, [4105, 4105, 4105]), (1.0, [4109, 4109, 8999])):
+        tok, acc, logp, ws = rlk.draft_verify(**a, u_sample=torch.full((3,), u, device="cuda"))
+        assert rlk.check_status(ws) == 0 and tok.tolist() == want, (u, tok)
+        ref = torch.log_softmax(z.double(), 1)[range(3), want]
+        assert torch.all((logp.double() - ref).abs() <= 2.0 ** -23 * ref.abs())
+    z[0, 8500] = float("nan")
+    tok, acc, logp, ws = rlk.draft_verify(**a, u_sample=torch.full((3,), 0.55, device="cuda"))
+    assert rlk.check_status(ws) == rlk.DERR_LOGITS and tok.tolist() == [-1, 4105, 4105]
+
+
 def test_verify_reports_bad_rows():
     def status(**over):
         a = verify_inputs([2, 2], 5000, "f32", True, 6, 1.0)
