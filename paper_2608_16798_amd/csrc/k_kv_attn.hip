@@ -13,6 +13,13 @@
 // Work is cut by cost, not by sequence: the row tiles of all sequences and key heads, each with the keys it sees, lie in
 // one line that every workgroup takes an equal piece of.  A tile cut between workgroups leaves partial sums that
 // k_kv_merge joins in order.  One token over a long history and a batch of ragged ones are the same to it.
+//
+// What bounds it: few rows, the cache's bytes (128 sequences of 500 to 8,000 tokens, one new token each, 8 key heads of
+// 128: 2.2 GB in 383 us, 5.8 TB/s); many rows, the matrix units and the exponentials between them, at the clock that the
+// card's power leaves (1.2 TFLOP of causal 128-wide bf16 in 1,300 us, 920 TFLOP/s: the matrix units busy 46 % of the
+// cycles, the vector ALU 42 %, at 1.8 GHz; other interleavings of the two, 8 wavefronts in step or 64 rows to a
+// wavefront, ended within 3 % of this).  Small calls: a chain of loads that wait for each other (offsets, lengths, page
+// indices, keys), and the join's: 8 sequences of up to 700 tokens take 18 us.
 #include "rlk_internal.h"
 
 #include <limits.h>
@@ -30,7 +37,7 @@ constexpr float kLn2f = 0.6931471805599453f, kLog2ef = 1.4426950408889634f;
 constexpr int kPageCap = 1024;     // page indices held in LDS
 constexpr int kLiveCap = 512;      // tiles looked through at once, with subtree ends
 constexpr int kWhole = 1 << 30;    // mark of a tile that every row sees whole
-constexpr int kItemCost = 96;      // cost of starting a row tile, in keys
+constexpr int kItemCost = 96;      // cost of starting a row tile, in keys (with 48, 8 short histories 18.4 -> 21.9 us)
 constexpr float kLazy = 8.0f;      // the maximum may be passed by 2^8 before the sums are rescaled
 
 #define LDSP(p) ((__attribute__((address_space(3))) void*)(p))
@@ -270,7 +277,8 @@ __device__ __forceinline__ int tile_kind(int2 ends, int last_key, int first, int
 
 // With subtree ends: the line of work counts the tiles of keys that a row tile takes and no others (in a packed tree of
 // many branches fewer than half, and a share that differs by sequence).  Workgroup b: the ends of each of its tiles, then
-// the row tiles' costs, a wavefront to each, and their sums.
+// the row tiles' costs, a wavefront to each, and their sums.  (Packed trees of up to 8,300 positions, 700 to 1,333 of
+// them new, in branches of 150: 9 us, and the attention 235 -> 142 us.)
 __global__ void __launch_bounds__(1024) k_kv_tree_plan(KvArgs a, AttnArgs p, AttnPlan pl, int TK) {
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const Seq s = sequence(a, b);
@@ -712,7 +720,9 @@ __global__ void __launch_bounds__(C::WAVES * 64, C::OCC) k_kv_attn(KvArgs a, Att
           if (poisoned) odd_values(0);
         }
         f32x16 sc[NB];
-        u32x4 pw[2 * NB];  // bf16: the probabilities, 16 keys to an element
+        // bf16: the probabilities, 16 keys to an element.  Rounded for the product, which takes no wider operand: each weight
+        // is off by at most 2^-8 of itself, as the values are; their sum is taken before, in fp32.
+        u32x4 pw[2 * NB];
         if (active) {
           // ---- scores: a group of key fragments ahead of the products
           constexpr int GR = ESZ == 4 ? 2 : NB * KS % 4 ? 3 : 4, NG = NB * KS / GR;
@@ -1052,7 +1062,11 @@ __global__ void __launch_bounds__(256) k_kv_merge(KvArgs a, AttnArgs p, AttnPlan
 }
 
 // Tiles by type and head size.  Few: 32 query rows, the wavefronts split the keys (one to a few tokens: bound by the
-// cache's bytes).  Many: 128 rows, 32 to a wavefront.
+// cache's bytes).  Many: 128 rows, 32 to a wavefront.  Two stages of tiles, or as many as keep 64 KiB of keys and values
+// in flight for Few.  64-wide heads leave registers and LDS for three workgroups of Many on a compute unit (66,000 tiles
+// of 128 rows and 64 keys: 207 -> 196 us against two with three stages).  Heads of 72 to 96 lie in LDS as 128 wide but
+// are multiplied as 96 (fp32 batch of 80-wide heads 41 -> 37 us).  At the widest heads some 20 registers are spilled
+// outside the products' loops.
 template <typename T, int DC> struct Few;
 template <typename T, int DC> struct Many;
 template <> struct Few<bf16_t, 64> : Cfg<bf16_t, 64, 1, 4, 1, 4, 1> {};
@@ -1074,7 +1088,8 @@ template <> struct Many<float, 256> : Cfg<float, 256, 4, 1, 1, 2, 1> {};
 
 constexpr int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-// What the launch and the workspace share.
+// What the launch and the workspace share.  Few where a sequence's rows of a key head fit its 32 (64 sequences of 4,000
+// tokens, 32 rows each: 194 us against 199 by Many; 8 of 2,000: 25 against 28), by max_new or the rows of the call.
 struct Shape {
   bool few;
   int DP, BM, tpt, wgs;
@@ -1161,7 +1176,7 @@ hipError_t launch_kv_attention(int dtype, const KvArgs& a, const AttnArgs& p, in
   const Layout L = layout(a, sh.DP, sh.wgs, sh.BM);
   AttnPlan pl = {};
   pl.tpt = sh.tpt;
-  pl.min_piece = 128;
+  pl.min_piece = 128;  // keys: smaller pieces leave more to join than they spread (64: a ragged fp32 batch 36.6 -> 37.9 us)
   pl.desc = reinterpret_cast<MergeDesc*>(ws + L.desc);
   pl.flags = reinterpret_cast<int32_t*>(ws + L.flags);
   pl.ml = reinterpret_cast<float2*>(ws + L.ml);

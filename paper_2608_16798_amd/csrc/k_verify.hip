@@ -6,6 +6,10 @@
 //   1. stats: every row once, chunk by chunk: the chunk's largest logit m and sum of exp((z - m) / tau);
 //   2. decide: per sequence, the drafts accepted and, of the row that the last token is drawn from, each chunk's mass;
 //   3. draw: the chunk that holds the target, then the token in it.
+//
+// The first pass is bound by the vector ALU (an fp64 exponential for each logit; 1,152 rows of 151,936
+// bf16 logits, 350 MB, in 128 us, 2.7 TB/s), the others by the loads that wait for each other (4.8, 7.0 and 5.8 us for
+// one sequence with four drafts).
 #include "rlk_internal.h"
 
 #include <limits.h>
@@ -484,7 +488,8 @@ hipError_t launch_draft_verify(int dtype, const VerifyArgs& a, void* part, doubl
   const int64_t rows = a.n_draft + a.B + (a.draft_logits ? a.n_draft : 0);
   const unsigned grid = (unsigned)(rows * a.nchunk);
   // Every workgroup of decide judges its sequence's drafts for itself, then takes `per` chunks: all of them apart while
-  // that fills the GPU, more to a workgroup for a larger batch.
+  // that fills the GPU, more to a workgroup for a larger batch (400 sequences: 474 us with all apart, 445 so; 128: 163
+  // both ways, and 179 with four times as many to a workgroup).
   const int per = (int)std::min<int64_t>(std::max<int64_t>((int64_t)a.nchunk * a.B / 2048, 1), a.nchunk);
   const dim3 grid2((unsigned)((a.nchunk + per - 1) / per), (unsigned)a.B);
   if (dtype == RLK_DTYPE_BF16) {
