@@ -1063,7 +1063,8 @@ __global__ void __launch_bounds__(256) k_kv_merge(KvArgs a, AttnArgs p, AttnPlan
 
 // Tiles by type and head size.  Few: 32 query rows, the wavefronts split the keys (one to a few tokens: bound by the
 // cache's bytes).  Many: 128 rows, 32 to a wavefront.  Two stages of tiles, or as many as keep 64 KiB of keys and values
-// in flight for Few.  64-wide heads leave registers and LDS for three workgroups of Many on a compute unit (66,000 tiles
+// in flight for Few; but Few's fp32 heads above 64, bound by the matrix units' fp32 rate, take one stage and twice the
+// wavefronts (16 sequences of 100 to 3,000 tokens of 8 128-wide heads: 88 -> 65 us).  64-wide heads leave registers and LDS for three workgroups of Many on a compute unit (66,000 tiles
 // of 128 rows and 64 keys: 207 -> 196 us against two with three stages).  Heads of 72 to 96 lie in LDS as 128 wide but
 // are multiplied as 96 (fp32 batch of 80-wide heads 41 -> 37 us).  At the widest heads some 20 registers are spilled
 // outside the products' loops.
@@ -1074,9 +1075,9 @@ template <> struct Few<bf16_t, 96> : Cfg<bf16_t, 128, 1, 4, 1, 2, 1, 96> {};
 template <> struct Few<bf16_t, 128> : Cfg<bf16_t, 128, 1, 4, 1, 2, 1> {};
 template <> struct Few<bf16_t, 256> : Cfg<bf16_t, 256, 1, 2, 1, 2, 1> {};
 template <> struct Few<float, 64> : Cfg<float, 64, 1, 4, 1, 2, 1> {};
-template <> struct Few<float, 96> : Cfg<float, 128, 1, 2, 1, 2, 1, 96> {};
-template <> struct Few<float, 128> : Cfg<float, 128, 1, 2, 1, 2, 1> {};
-template <> struct Few<float, 256> : Cfg<float, 256, 1, 1, 1, 2, 1> {};
+template <> struct Few<float, 96> : Cfg<float, 128, 1, 4, 1, 1, 1, 96> {};
+template <> struct Few<float, 128> : Cfg<float, 128, 1, 4, 1, 1, 1> {};
+template <> struct Few<float, 256> : Cfg<float, 256, 1, 2, 1, 1, 1> {};
 template <> struct Many<bf16_t, 64> : Cfg<bf16_t, 64, 4, 1, 2, 2, 3> {};
 template <> struct Many<bf16_t, 96> : Cfg<bf16_t, 128, 4, 1, 2, 2, 2, 96> {};
 template <> struct Many<bf16_t, 128> : Cfg<bf16_t, 128, 4, 1, 2, 2, 2> {};
