@@ -102,7 +102,8 @@ def build(verbose: bool = True, sanitize: bool = False) -> str:
     return lib
 
 
-HOST_TESTS = ["tests/test_abi.py", "tests/test_tree_pack.py", "tests/test_binding_args.py"]
+HOST_TESTS = ["tests/test_abi.py", "tests/test_tree_pack.py", "tests/test_binding_args.py", "tests/test_rollout_args.py",
+              "tests/test_rollout_oracle.py"]
 
 
 def run_host_sanitizers() -> int:

@@ -495,6 +495,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, C::OCC) k_kv_attn(KvArgs a, Att
     const int wg_first = ctx + tok0, wg_last = ctx + tok0 + ntok - 1;       // slots of the workgroup's rows
     const int first_slot = ctx + tok0 + min((wm * 32) / g, ntok - 1);       // of the wavefront's
     const int last_slot = ctx + tok0 + min((wm * 32 + 31) / g, ntok - 1);
+    const bool rows_here = wm * 32 < ntok * g;  // a wavefront without a row only copies
     u32x4 qf[KS];
     {
       const T* q = (const T*)p.q + (int64_t)(s.row0 + tok0 + rtok) * p.q_stride + (int64_t)(h * g + row % g) * a.D;
@@ -677,7 +678,7 @@ __global__ void __launch_bounds__(C::WAVES * 64, C::OCC) k_kv_attn(KvArgs a, Att
           some_after = __any(e > first_slot);
           all_wg = __all(e > wg_last);
         }
-        const bool active = part0 <= last_slot && some_after;
+        const bool active = rows_here && part0 <= last_slot && some_after;
         const bool odd_matters = !(part0 + C::PK - 1 <= wg_first && all_wg) && part0 <= wg_last;
         const char* kst = smem + stage * C::STAGE;
         if (odd_matters) {
@@ -1064,10 +1065,10 @@ __global__ void __launch_bounds__(256) k_kv_merge(KvArgs a, AttnArgs p, AttnPlan
 // Tiles by type and head size.  Few: 32 query rows, the wavefronts split the keys (one to a few tokens: bound by the
 // cache's bytes).  Many: 128 rows, 32 to a wavefront.  Two stages of tiles, or as many as keep 64 KiB of keys and values
 // in flight for Few; but Few's fp32 heads above 64, bound by the matrix units' fp32 rate, take one stage and twice the
-// wavefronts (16 sequences of 100 to 3,000 tokens of 8 128-wide heads: 88 -> 65 us).  64-wide heads leave registers and LDS for three workgroups of Many on a compute unit (66,000 tiles
-// of 128 rows and 64 keys: 207 -> 196 us against two with three stages).  Heads of 72 to 96 lie in LDS as 128 wide but
-// are multiplied as 96 (fp32 batch of 80-wide heads 41 -> 37 us).  At the widest heads some 20 registers are spilled
-// outside the products' loops.
+// wavefronts (16 sequences of 100 to 3,000 tokens of 8 128-wide heads: 88 -> 65 us).  64-wide bf16 heads leave registers
+// and LDS for three workgroups of Many on a compute unit (61,000 tiles of 128 rows and 64 keys: 207 -> 196 us against two
+// with three stages).  Heads of 72 to 96 lie in LDS as 128 wide but are multiplied as 96 (fp32 batch of 80-wide heads
+// 41 -> 37 us).  At the widest heads some 20 registers are spilled outside the products' loops.
 template <typename T, int DC> struct Few;
 template <typename T, int DC> struct Many;
 template <> struct Few<bf16_t, 64> : Cfg<bf16_t, 64, 1, 4, 1, 4, 1> {};
