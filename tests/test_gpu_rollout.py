@@ -269,6 +269,24 @@ def test_attention_of_many_sequences(H, K, B):
         check_attention(c, table, lens, cu, q, "bf16", 0.25, ends=ends, max_new=hint, tag=f"trees, hint {hint}")
 
 
+def test_attention_of_the_most_sequences():
+    """16,384 sequences, the most of a call, of no token to three, one new token in each that has one."""
+    rng = np.random.default_rng(3)
+    seqs = [(int(rng.integers(0, 3)), int(rng.random() < 0.9)) for _ in range(16384)]
+    c, table, lens, cu, gen = build(seqs, 1, 4, 8, "f32", seed=3, extra_cols=0)
+    q = torch.randn(int(cu[-1]), 1, 8, generator=gen, device="cuda")
+    check_attention(c, table, lens, cu, q, "f32", 0.35, max_new=1, tag="causal")
+    check_attention(c, table, lens, cu, q, "f32", 0.35, ends=np.tile([3, 2, 3], (16384, 1)), max_new=1, tag="trees")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_of_a_long_chunk(dtype):
+    """A prompt of 5,003 tokens at once beside a single token: every row tile from the first key on, cut many times."""
+    c, table, lens, cu, gen = build([(0, 5003), (70, 1)], 1, 32, 16, dtype, seed=8)
+    q = torch.randn(int(cu[-1]), 2, 16, generator=gen, device="cuda").to(DT[dtype])
+    check_attention(c, table, lens, cu, q, dtype, 0.25, tag="causal")
+
+
 @pytest.mark.parametrize("ps", [2, 8, 64])
 @pytest.mark.parametrize("new", [3, 70])
 def test_attention_over_long_trees(ps, new):
@@ -644,6 +662,57 @@ def test_graph_replay(new):
     torch.cuda.synchronize()
     for n, t in o.items():
         assert torch.equal(t, ref2[n]), n
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_captured_step_follows_growing_lengths(tree):
+    """One decoding step captured with its lengths on the device: every replay appends a token further, over page and
+    tile ends, and gives what eager calls on a cache of their own give."""
+    seqs = [(61, 1), (0, 1), (127, 1), (15, 1)]
+    steps = 40
+
+    def made():
+        c, table, lens, cu, gen = build([(n + steps, 1) for n, _ in seqs], 2, 16, 64, "bf16", 21, fill=0.0)
+        c["kv_len"] = dev([n + k for n, k in seqs])
+        q, k, v = (torch.randn(4, h, 64, generator=gen, device="cuda").to(torch.bfloat16) for h in (4, 2, 2))
+        ends = torch.full((4, 200), 1000, dtype=torch.int32, device="cuda") if tree else None
+        if tree:
+            ends[:, 7:40] = 40  # a branch that is over once a sequence has passed 40 tokens
+        o = dict(q=torch.empty_like(q), out=torch.empty_like(q), lse=torch.empty(4, 4, device="cuda"))
+        freq = 1e4 ** (-torch.arange(32, dtype=torch.float64, device="cuda") / 32)
+        b = rlk.make_cache(**c, T=4, n_q_heads=4)
+        ws = rlk.alloc_workspace(rlk.kv_workspace_size(b))
+
+        def step():
+            rlk.kv_append(**c, q=q, k=k, v=v, freq=freq, q_out=o["q"], ws=ws)
+            rlk.kv_attention(o["q"], **c, slot_end=ends, out=o["out"], lse=o["lse"], max_new=1, ws=ws)
+            c["kv_len"].add_(1)
+            k.mul_(0.97)
+
+        return step, o, c, ws
+
+    eager, eo, ec, ews = made()
+    captured, go, gc, gws = made()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        eager()
+        captured()  # the first step of both
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        captured()
+    for i in range(1, steps):
+        eager()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert rlk.check_status(ews) == 0 and rlk.check_status(gws) == 0
+        for n in eo:
+            assert torch.equal(eo[n], go[n]), (i, n)
+    assert torch.equal(ec["k_pages"], gc["k_pages"]) and torch.equal(ec["v_pages"], gc["v_pages"])
+    assert torch.equal(ec["kv_len"], gc["kv_len"])
 
 
 def test_two_graphs_share_a_workspace():
