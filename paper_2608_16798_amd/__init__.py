@@ -789,6 +789,17 @@ def _on_device(t, call, stream):
     return call(torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """An uninitialised tensor for a call on `stream` (None: the current one): allocated there, so that its memory is
+    neither still in use by another stream's earlier work nor handed to another stream while the call runs."""
+    import torch
+
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def kv_append(k_pages, v_pages, page_table, kv_len, cu_new, q, k, v, freq=None, positions=None, q_norm=None, k_norm=None,
               norm_eps: float = 1e-6, rot_style: str = "half", q_out=None, ws=None, stream=None):
     """Appends new tokens' keys and values to the paged cache, normed and rotated on the way, and makes their
@@ -824,9 +835,9 @@ def kv_append(k_pages, v_pages, page_table, kv_len, cu_new, q, k, v, freq=None, 
                  rot_style=ROT_PAIRS if rot_style == "pairs" else ROT_HALF, q_norm=_ptr(q_norm), k_norm=_ptr(k_norm),
                  norm_eps=norm_eps)
     if q is not None and q_out is None:
-        q_out = torch.empty(T, Hq, D, dtype=dt, device=q.device)
+        q_out = _empty((T, Hq, D), dt, q.device, stream)
     if ws is None:
-        ws = alloc_workspace(kv_workspace_size(c), k_pages.device)
+        ws = _empty(kv_workspace_size(c), torch.uint8, k_pages.device, stream)
     _check(_on_device(k_pages, lambda s: lib.rlk_kv_append(
         ctypes.byref(c), ctypes.byref(r), _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(positions), _ptr(q_out), _ptr(ws),
         ws.numel(), s), stream))
@@ -854,9 +865,9 @@ def kv_attention(q, k_pages, v_pages, page_table, kv_len, cu_new, scale=None, sl
     lib = load_library()
     c = make_cache(k_pages, v_pages, page_table, kv_len, cu_new, T, Hq, max_new)
     if out is None:
-        out = torch.empty(T, Hq, D, dtype=dt, device=q.device)
+        out = _empty((T, Hq, D), dt, q.device, stream)
     if ws is None:
-        ws = alloc_workspace(kv_workspace_size(c), q.device)
+        ws = _empty(kv_workspace_size(c), torch.uint8, q.device, stream)
     _check(_on_device(q, lambda s: lib.rlk_kv_attention(
         ctypes.byref(c), _ptr(q), qs, _ptr(slot_end), 0 if slot_end is None else slot_end.shape[1],
         D ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), s), stream))
@@ -899,13 +910,13 @@ def draft_verify(logits, draft, cu_draft, u_accept, u_sample, draft_logits=None,
     dev = logits.device
     p = Verify(n_draft=n, B=B, V=V, dtype=_dtype_code(logits), temperature=temperature, ld_logits=V, ld_draft=V)
     if tokens is None:
-        tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+        tokens = _empty(rows, torch.int32, dev, stream)
     if n_accepted is None:
-        n_accepted = torch.empty(B, dtype=torch.int32, device=dev)
+        n_accepted = _empty(B, torch.int32, dev, stream)
     if logp is None:
-        logp = torch.empty(rows, dtype=torch.float32, device=dev)
+        logp = _empty(rows, torch.float32, dev, stream)
     if ws is None:
-        ws = alloc_workspace(verify_workspace_size(p), dev)
+        ws = _empty(verify_workspace_size(p), torch.uint8, dev, stream)
     _check(_on_device(logits, lambda s: lib.rlk_draft_verify(
         ctypes.byref(p), _ptr(logits), _ptr(draft_logits), _ptr(draft), _ptr(cu_draft), _ptr(u_accept), _ptr(u_sample),
         _ptr(tokens), _ptr(n_accepted), _ptr(logp), _ptr(ws), ws.numel(), s), stream))

@@ -773,6 +773,24 @@ def test_two_streams():
             assert torch.equal(t, ref[n]), n
 
 
+def test_what_a_call_on_another_stream_allocates_belongs_to_that_stream():
+    """Outputs and workspaces that a call makes itself: once dropped, their memory is not the current stream's to reuse
+    while the call may still run."""
+    c, table, lens, cu, gen = build([(70, 3), (9, 1)], 2, 16, 64, "bf16", 4)
+    q, k, v = (torch.randn(4, h, 64, generator=gen, device="cuda").to(torch.bfloat16) for h in (4, 2, 2))
+    a = verify_inputs([3, 0], 5001, "bf16", True, 2, 1.0)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for call in (lambda: rlk.kv_append(**c, q=q, k=k, v=v, stream=side), lambda: rlk.kv_attention(q, **c, stream=side),
+                 lambda: rlk.draft_verify(**a, stream=side)):
+        got = [t for t in call() if t is not None]
+        sizes = [(t.data_ptr(), t.numel() * t.element_size()) for t in got]
+        del got
+        here = [torch.empty(n, dtype=torch.uint8, device="cuda") for _, n in sizes]
+        assert not {t.data_ptr() for t in here} & {at for at, _ in sizes}
+        torch.cuda.synchronize()
+
+
 # ---- run together ----
 
 def test_packed_tree_through_the_cache_gives_each_trajectory_its_log_probs():
